@@ -31,8 +31,8 @@ typedef enum {
     EOSQ_WARN_BLOCK_STATUS = 5     /* only from eosq_check_status: some block raised a flag */
 } eosq_status;
 
-/* Input / output element types. */
-enum { EOSQ_F16 = 0, EOSQ_F32 = 1 };
+/* Input / output element types.  EOSQ_BF16 is taken by the 8-bit paged cache only. */
+enum { EOSQ_F16 = 0, EOSQ_F32 = 1, EOSQ_BF16 = 2 };
 
 /* Capacity of the per-block factor arrays.  The rank test of Algorithm 2 cannot return more than
  * the pilot k (= 11 at d = 128) outliers, because its bulk-edge estimate is at least lambda_{k+1}. */
@@ -195,6 +195,132 @@ int eosq_scores(eosq_ctx *ctx, const eosq_cache_t *kcache, int64_t num_kv_heads,
                 int64_t blocks_per_head, int64_t head_stride_blocks, int n, int d, int bits,
                 uint64_t seed, const void *q, int G, float scale, float *scores, void *cuda_stream);
 
+/* ---- 8-bit paged cache --------------------------------------------------------------------
+ *
+ * Keys and values of tokens that no compressed block holds: the newest tokens of a sequence, the tokens that a
+ * block is still being filled with, or an encoder's states.  (The paper keeps such tokens as they are, in an
+ * fp16 tail buffer next to the compressed blocks.)  A number is held as one byte, its code; the tokens of a
+ * page share, per KV head, one scale for their keys and one for their values: number = code * scale.
+ *
+ * Sequences own pages through a table in device memory; whole pages may be shared by several sequences (after
+ * eosq_kv8_fork), a page that is not full belongs to one.  All state is plain device memory of the caller.
+ * Every call below enqueues kernels on the given stream, allocates nothing, does not synchronise and can be captured
+ * into a graph.  Calls that use the same cache or the same workspace must be ordered among themselves.
+ *
+ * Numbers in device memory (table, lengths, lists of sequences, offsets) are checked by the kernels: an entry that makes no
+ * sense is skipped, nothing out of bounds is read or written, and a bit of *flags is raised (eosq_kv8_check).
+ */
+enum { EOSQ_KV_INT8 = 0, EOSQ_KV_E4M3 = 1 };
+
+typedef struct {
+    uint8_t *k, *v;            /* [layers][num_pages][kv_heads][page_size][d] codes: int8, or e4m3 without its NaNs   */
+    float *k_scale, *v_scale;  /* [layers][num_pages][kv_heads] positive, 2^-64 .. 2^64                               */
+    int32_t *table;            /* [max_seqs][max_pages] page of each page_size tokens of a sequence, -1: none         */
+    int32_t *lengths;          /* [max_seqs] tokens of each sequence, 0: empty                                        */
+    int32_t *refs;             /* [num_pages] table entries that name a page, 0: the page is free                     */
+    int32_t *flags;            /* [1] EOSQ_KV8_* bits, raised by the calls below                                      */
+    int32_t layers, num_pages, kv_heads;
+    int32_t page_size;         /* 16, 32, 64 or 128 tokens */
+    int32_t d;                 /* 64 or 128 */
+    int32_t format;            /* EOSQ_KV_INT8 or EOSQ_KV_E4M3 */
+    int32_t max_seqs, max_pages;
+} eosq_kv8_t;
+
+/* Bits of *flags. */
+#define EOSQ_KV8_NO_PAGE 1u    /* reserve / fork: the pool had too few free pages for an entry                        */
+#define EOSQ_KV8_TOO_LONG 2u   /* reserve: a sequence would not fit its row of the table                              */
+#define EOSQ_KV8_BAD_SEQ 4u    /* a sequence outside 0 .. max_seqs-1, listed twice, with a senseless length or offset;
+                                  fork: a destination that is not empty                                               */
+#define EOSQ_KV8_BAD_PAGE 8u   /* a table entry outside the pool, or a count of table entries that does not add up    */
+
+/* Most sequences of a cache, and of one call's list. */
+#define EOSQ_KV8_MAX_SEQS 8192
+
+/* Scratch bytes of the calls below for this cache (256-byte aligned dev memory; contents need not be kept between calls, one call
+ * at a time).  query_rows: for eosq_kv8_attend the most query rows that a KV head of one sequence has, max_q * G; 0 for
+ * the others.  0 if the geometry is not supported. */
+size_t eosq_kv8_workspace_bytes(const eosq_kv8_t *cache, int query_rows);
+
+/*
+ * Room for add[i] more tokens of sequence seqs[i], i = 0 .. n-1 in this order (dev int32 arrays): its length grows by add[i],
+ * the pages that it lacks are the lowest free ones.  first[i] (dev) gets the position of the first new token, the old length;
+ * -1 if the entry was refused (then nothing of it changed): no pages, no room in its row, a bad sequence or one that is listed
+ * a second time, add[i] < 0.  An entry that pages do not reach for is refused, and so is every later one that needs
+ * any.  A sequence of -1 is skipped without a flag (padding), here and in the calls below.
+ */
+int eosq_kv8_reserve(eosq_ctx *ctx, const eosq_kv8_t *cache, const int32_t *seqs, const int32_t *add, int n, int32_t *first,
+                     void *cuda_stream);
+
+/*
+ * Quantises new tokens into the pages of one layer.  Entry i's tokens are rows cu[i] .. cu[i+1]-1 of `k` and `v`
+ * and go to positions first[i], first[i]+1, ... of sequence seqs[i], all below its length (what eosq_kv8_reserve returned; an
+ * entry with first[i] < 0 is skipped).
+ *   k, v   dev [total][kv_heads][d] of dtype EOSQ_F16, EOSQ_BF16 or EOSQ_F32; token and head strides in elements, d contiguous;
+ *          base and strides multiples of 16 bytes
+ *   max_new  host, at least the largest cu[i+1] - cu[i]
+ * With a the largest finite magnitude among the new values of a page and head:
+ *   EOSQ_KV_INT8: s = a / 127 rounded to fp32;  EOSQ_KV_E4M3: s = the least power of two with a <= 448 s;
+ * both held to 2^-64 .. 2^64.  A page whose first new token is not its first token keeps the larger of s and its old scale, and
+ * if that is s its older codes c become round(c * s_old / s).  New codes are round(x / scale): of the exact quotient, half to
+ * even, saturated; NaN becomes 0.  Tokens of a page behind the last new one are not touched.  A sequence is listed once, and
+ * what is written belongs to it alone.
+ */
+int eosq_kv8_store(eosq_ctx *ctx, const eosq_kv8_t *cache, int layer, const void *k, const void *v, int dtype, int64_t total,
+                   int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride,
+                   const int32_t *seqs, const int32_t *first, const int32_t *cu, int n, int max_new, void *cuda_stream);
+
+/*
+ * Attention over the cached tokens of one layer.  Entry i's queries are rows cu[i] .. cu[i+1]-1 of q: m of them, for the last m
+ * positions of sequence seqs[i] (length len): query t stands at position p = len - m + t.  Query head g of KV head h is head
+ * h*G + g.  A query sees the tokens j with
+ *   causal != 0:  j <= p, and j > p - window if window > 0;      causal == 0 (window must be 0):  every j < len
+ * (cross attention to an encoder's states, of any number).  With s_j = scale * <q, k_j> over what it sees,
+ *   out = sum_j exp(s_j) v_j / sum_j exp(s_j),   lse = log sum_j exp(s_j);   seeing nothing: out = 0, lse = -infinity.
+ *   q, out  dev [total][kv_heads*G][d], both of dtype EOSQ_F16 or EOSQ_BF16; token and head strides in elements, d contiguous, base
+ *           and strides multiples of 16 bytes; q and out do not overlap
+ *   lse     dev fp32 [total][kv_heads*G], or null
+ *   max_q   host, at least the largest cu[i+1] - cu[i]; an entry with more is skipped
+ *   workspace  eosq_kv8_workspace_bytes(cache, max_q*G)
+ * Rows that belong to no entry (behind cu[n], or of a sequence of -1) are left as they are.  Sums and the statistics are held in fp32;
+ * weights are rounded to fp16 before they meet the values.  `lse` lets a caller join the result with attention over other tokens
+ * of the sequence.
+ */
+int eosq_kv8_attend(eosq_ctx *ctx, const eosq_kv8_t *cache, int layer, const void *q, int dtype, int64_t total,
+                    int64_t q_token_stride, int64_t q_head_stride, const int32_t *seqs, const int32_t *cu, int n, int max_q, int G,
+                    float scale, int causal, int window, void *out, int64_t out_token_stride, int64_t out_head_stride, float *lse,
+                    void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Sequence dst[i] becomes a copy of sequence src[i] as it was before the call, i = 0 .. n-1 (dev int32 arrays): they share its whole pages, a last page
+ * that is not full is copied, in all layers, to the lowest free page.  A destination is empty and listed once (else the entry is
+ * refused and raises a flag: it stays empty); a source may be listed more than once.
+ */
+int eosq_kv8_fork(eosq_ctx *ctx, const eosq_kv8_t *cache, const int32_t *src, const int32_t *dst, int n, void *workspace,
+                  size_t workspace_bytes, void *cuda_stream);
+
+/* Empties the listed sequences: their table entries become -1, their lengths 0, and pages that nobody else names are free again.
+ * Listing a sequence twice empties it once (and raises a flag); an empty one stays as it is. */
+int eosq_kv8_free(eosq_ctx *ctx, const eosq_kv8_t *cache, const int32_t *seqs, int n, void *cuda_stream);
+
+/*
+ * Moves the used pages to the front of the pool: with L of them, the used pages at L and beyond, in ascending order, go to the free
+ * ones below L, in ascending order; the others stay.  The table and refs follow.  remap (dev int32 [num_pages]) gets each
+ * page's place, -1 for a page that was free.
+ */
+int eosq_kv8_compact(eosq_ctx *ctx, const eosq_kv8_t *cache, int32_t *remap, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Copies pages src_pages[i] of `from` to dst_pages[i] of `to`, codes and scales of all layers (dev int32 arrays): to another pool of the
+ * same geometry, or within one.  Tables and refs are the caller's business.  A destination is listed once and is no
+ * source of the same call.
+ */
+int eosq_kv8_copy_pages(eosq_ctx *ctx, const eosq_kv8_t *from, const eosq_kv8_t *to, const int32_t *src_pages, const int32_t *dst_pages,
+                        int n, void *cuda_stream);
+
+/* Synchronises the stream and puts the cache's flags into *flags (host), clearing them.  Returns EOSQ_WARN_BLOCK_STATUS if any was
+ * raised, EOSQ_ERR_CUDA as eosq_check_status does (kernel bit 64: attention), EOSQ_OK otherwise. */
+int eosq_kv8_check(eosq_ctx *ctx, const eosq_kv8_t *cache, uint32_t *flags, void *cuda_stream);
+
 /*
  * Host-buffer convenience for end-to-end use: copies `blocks` (host, pinned preferred) to the
  * device in chunks, encodes, and copies codes, norms, rank, sigma, phi, P, V and status back into
@@ -213,7 +339,7 @@ int eosq_encode_host(eosq_ctx *ctx, const void *host_blocks, int in_dtype, int64
  * words (dev) is non-zero, EOSQ_OK otherwise; *flagged (host, may be null) gets the count.
  * If a kernel launched through the context has given up a bounded device-side wait since the last
  * call (its outputs are then incomplete), returns EOSQ_ERR_CUDA instead, with the kernels' bits in
- * eosq_last_cuda_error() (1 Gram, 2 quantise, 8 scores, 16 decode, 32 self-test), and clears that
+ * eosq_last_cuda_error() (1 Gram, 2 quantise, 8 scores, 16 decode, 32 self-test, 64 attention), and clears that
  * record: it is reported once and the context stays usable. */
 int eosq_check_status(eosq_ctx *ctx, const int32_t *status, int64_t num_blocks, int64_t *flagged,
                       void *cuda_stream);

@@ -18,7 +18,9 @@ _PKG = Path(__file__).resolve().parent
 LIB_PATH = _PKG / "libeosq.so"
 
 EOSQ_OK, EOSQ_ERR_INVALID_ARG, EOSQ_ERR_UNSUPPORTED, EOSQ_ERR_BUFFER_TOO_SMALL, EOSQ_ERR_CUDA, EOSQ_WARN_BLOCK_STATUS = range(6)
-EOSQ_F16, EOSQ_F32 = 0, 1
+EOSQ_F16, EOSQ_F32, EOSQ_BF16 = 0, 1, 2
+EOSQ_KV_INT8, EOSQ_KV_E4M3 = 0, 1
+EOSQ_KV8_NO_PAGE, EOSQ_KV8_TOO_LONG, EOSQ_KV8_BAD_SEQ, EOSQ_KV8_BAD_PAGE = 1, 2, 4, 8
 EOSQ_RMAX = 16
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "UNSUPPORTED", 3: "BUFFER_TOO_SMALL", 4: "CUDA", 5: "BLOCK_STATUS"}
 
@@ -28,6 +30,8 @@ EXPORTS = [
     "eosq_decode", "eosq_scores", "eosq_encode_host_arena_bytes", "eosq_encode_host",
     "eosq_check_status", "eosq_launch_count", "eosq_profile_enable", "eosq_profile_select", "eosq_profile_read",
     "eosq_encode_static", "eosq_encode_static_max_blocks", "eosq_selftest_wait_timeout",
+    "eosq_kv8_workspace_bytes", "eosq_kv8_reserve", "eosq_kv8_store", "eosq_kv8_attend", "eosq_kv8_fork", "eosq_kv8_free",
+    "eosq_kv8_compact", "eosq_kv8_copy_pages", "eosq_kv8_check",
 ]
 STAGES = ["gram", "tridiag_a", "tridiag_b", "tridiag_c", "eigvals", "spectral", "quant", "decode", "scores", "redo", "other"]
 
@@ -48,6 +52,11 @@ class _LayoutStruct(ctypes.Structure):
                 ("reserved", ctypes.c_int32)] + [
         (name, ctypes.c_int64) for name in
         ("codes_bytes", "norms_bytes", "P_bytes", "V_bytes", "sigma_bytes", "phi_bytes", "eig_bytes", "stored_bytes")]
+
+
+class _Kv8Struct(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("k", "v", "k_scale", "v_scale", "table", "lengths", "refs", "flags")] + [
+        (name, ctypes.c_int32) for name in ("layers", "num_pages", "kv_heads", "page_size", "d", "format", "max_seqs", "max_pages")]
 
 
 _lib = None
@@ -95,6 +104,18 @@ def lib():
         L.eosq_profile_select.argtypes = [ctypes.c_void_p, ctypes.c_uint32]
         L.eosq_profile_read.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
         L.eosq_check_status.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p]
+        p, i32, i64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64
+        L.eosq_kv8_workspace_bytes.restype = ctypes.c_size_t
+        L.eosq_kv8_workspace_bytes.argtypes = [p, i32]
+        L.eosq_kv8_reserve.argtypes = [p, p, p, p, i32, p, p]
+        L.eosq_kv8_store.argtypes = [p, p, i32, p, p, i32, i64, i64, i64, i64, i64, p, p, p, i32, i32, p]
+        L.eosq_kv8_attend.argtypes = [p, p, i32, p, i32, i64, i64, i64, p, p, i32, i32, i32, ctypes.c_float, i32, i32, p, i64, i64, p, p,
+                                      ctypes.c_size_t, p]
+        L.eosq_kv8_fork.argtypes = [p, p, p, p, i32, p, ctypes.c_size_t, p]
+        L.eosq_kv8_free.argtypes = [p, p, p, i32, p]
+        L.eosq_kv8_compact.argtypes = [p, p, p, p, ctypes.c_size_t, p]
+        L.eosq_kv8_copy_pages.argtypes = [p, p, p, p, p, i32, p]
+        L.eosq_kv8_check.argtypes = [p, p, p, p]
         _lib = L
     return _lib
 
@@ -354,3 +375,196 @@ def eosq_check_status(ctx: Context, cache: Cache, stream=None) -> int:
     if rc not in (EOSQ_OK, EOSQ_WARN_BLOCK_STATUS):
         _check(rc, "eosq_check_status", ctx)
     return int(flagged.value)
+
+
+# ---- 8-bit paged cache ---------------------------------------------------------------------
+
+class Kv8Cache:
+    """``eosq_kv8_t`` over torch tensors: keys and values of the tokens that no compressed block holds, a byte per number, in
+    pages that sequences own through a table in device memory.
+
+    k, v [layers][num_pages][kv_heads][page_size][d] uint8; k_scale, v_scale [layers][num_pages][kv_heads] float32; table
+    [max_seqs][max_pages], lengths [max_seqs], refs [num_pages] and flags [1] int32.  The attributes are the handle: they are set
+    once and cannot be replaced.  A new cache is empty: table -1, lengths, refs and flags 0."""
+
+    __slots__ = ("k", "v", "k_scale", "v_scale", "table", "lengths", "refs", "flags", "format", "layers", "num_pages", "kv_heads",
+                 "page_size", "d", "max_seqs", "max_pages", "device", "_struct", "_address")
+
+    def __init__(self, *, k, v, k_scale, v_scale, table, lengths, refs, format, flags=None):
+        import torch
+        if k.dim() != 5 or table.dim() != 2:
+            raise ValueError("k is [layers][num_pages][kv_heads][page_size][d], table [max_seqs][max_pages]")
+        layers, num_pages, kv_heads, page_size, d = k.shape
+        max_seqs, max_pages = table.shape
+        if flags is None:
+            flags = torch.zeros(1, dtype=torch.int32, device=k.device)
+        want = dict(k=(k, torch.uint8, tuple(k.shape)), v=(v, torch.uint8, tuple(k.shape)),
+                    k_scale=(k_scale, torch.float32, (layers, num_pages, kv_heads)), v_scale=(v_scale, torch.float32, (layers, num_pages, kv_heads)),
+                    table=(table, torch.int32, (max_seqs, max_pages)), lengths=(lengths, torch.int32, (max_seqs,)),
+                    refs=(refs, torch.int32, (num_pages,)), flags=(flags, torch.int32, (1,)))
+        st = _Kv8Struct()
+        for name, (t, dtype, shape) in want.items():
+            if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != k.device:
+                raise ValueError(f"{name}: {dtype} {list(shape)} contiguous on {k.device} is wanted, not {t.dtype} {list(t.shape)} on {t.device}")
+            object.__setattr__(self, name, t)
+            setattr(st, name, t.data_ptr())
+        for name, value in (("layers", layers), ("num_pages", num_pages), ("kv_heads", kv_heads), ("page_size", page_size), ("d", d),
+                            ("format", int(format)), ("max_seqs", max_seqs), ("max_pages", max_pages)):
+            object.__setattr__(self, name, value)
+            setattr(st, name, value)
+        object.__setattr__(self, "device", k.device)
+        object.__setattr__(self, "_struct", st)
+        object.__setattr__(self, "_address", ctypes.addressof(st))
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{name}: a Kv8Cache is made once; write into its tensors, or make another")
+
+    @staticmethod
+    def allocate(layers, num_pages, kv_heads, page_size, d, format, max_seqs, max_pages, device="cuda"):
+        import torch
+        shape = (layers, num_pages, kv_heads, page_size, d)
+        i32 = dict(dtype=torch.int32, device=device)
+        return Kv8Cache(k=torch.empty(shape, dtype=torch.uint8, device=device), v=torch.empty(shape, dtype=torch.uint8, device=device),
+                        k_scale=torch.ones(shape[:3], dtype=torch.float32, device=device), v_scale=torch.ones(shape[:3], dtype=torch.float32, device=device),
+                        table=torch.full((max_seqs, max_pages), -1, **i32), lengths=torch.zeros(max_seqs, **i32), refs=torch.zeros(num_pages, **i32),
+                        format=format)
+
+
+def _kv8_list(cache, t, n, what):
+    import torch
+    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.device != cache.device or (n is not None and t.shape[0] != n):
+        raise ValueError(f"{what}: int32 [{n if n is not None else 'n'}] contiguous on {cache.device} is wanted, not {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _kv8_rows(cache, t, heads, what):
+    """Data pointer and strides of [total][heads][d], d contiguous."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != cache.d or t.device != cache.device or t.stride(2) != 1:
+        raise ValueError(f"{what}: [total][{heads}][{cache.d}] with contiguous rows on {cache.device} is wanted, not {list(t.shape)} on {t.device}")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _any_dtype_code(t):
+    import torch
+    if t.dtype == torch.bfloat16:
+        return EOSQ_BF16
+    return _dtype_code(t)
+
+
+def _empty(shape, dtype, device, stream):
+    """New memory that belongs to the stream it is used on: freed, it goes back to that stream's later work."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _kv8_workspace(cache, rows, workspace, stream):
+    import torch
+    if workspace is None:
+        workspace = _empty(max(eosq_kv8_workspace_bytes(cache, rows), 256), torch.uint8, cache.device, stream)
+    elif workspace.device != cache.device or not workspace.is_contiguous():
+        raise ValueError(f"workspace: contiguous memory on {cache.device} is wanted")
+    return workspace
+
+
+def eosq_kv8_workspace_bytes(cache: Kv8Cache, query_rows: int = 0) -> int:
+    return int(lib().eosq_kv8_workspace_bytes(cache._address, int(query_rows)))
+
+
+def eosq_kv8_reserve(ctx: Context, cache: Kv8Cache, seqs, add, first=None, stream=None):
+    """Room for add[i] more tokens of sequence seqs[i].  Returns the position of each one's first new token, -1 where refused."""
+    import torch
+    n = seqs.shape[0]
+    if first is None:
+        first = _empty(n, torch.int32, cache.device, stream)
+    rc = lib().eosq_kv8_reserve(ctx._h, cache._address, _kv8_list(cache, seqs, None, "seqs"), _kv8_list(cache, add, n, "add"), n,
+                                _kv8_list(cache, first, n, "first"), _stream_ptr(stream))
+    _check(rc, "eosq_kv8_reserve", ctx)
+    return first
+
+
+def eosq_kv8_store(ctx: Context, cache: Kv8Cache, layer: int, k, v, seqs, first, cu, max_new: int, stream=None) -> None:
+    """k, v: [total][kv_heads][d] fp16, bf16 or fp32, any token and head strides that are multiples of 16 bytes."""
+    n = seqs.shape[0]
+    if k.dtype != v.dtype or k.shape[0] != v.shape[0]:
+        raise ValueError("k and v differ in type or number of tokens")
+    kp, kt, kh = _kv8_rows(cache, k, cache.kv_heads, "k")
+    vp, vt, vh = _kv8_rows(cache, v, cache.kv_heads, "v")
+    rc = lib().eosq_kv8_store(ctx._h, cache._address, layer, kp, vp, _any_dtype_code(k), k.shape[0], kt, kh, vt, vh, _kv8_list(cache, seqs, None, "seqs"),
+                              _kv8_list(cache, first, n, "first"), _kv8_list(cache, cu, n + 1, "cu"), n, max_new, _stream_ptr(stream))
+    _check(rc, "eosq_kv8_store", ctx)
+
+
+def eosq_kv8_attend(ctx: Context, cache: Kv8Cache, layer: int, q, seqs, cu, max_q: int, scale: Optional[float] = None, causal: bool = True,
+                    window: int = 0, out=None, lse=None, want_lse: bool = False, workspace=None, stream=None):
+    """q: [total][kv_heads * G][d] fp16 or bf16.  Returns out, or (out, lse) with want_lse (or with an lse to write to)."""
+    import torch
+    n, total, H = seqs.shape[0], q.shape[0], q.shape[1]
+    if H % cache.kv_heads or H == 0:
+        raise ValueError(f"q has {H} heads, not a multiple of {cache.kv_heads}")
+    G = H // cache.kv_heads
+    qp, qt, qh = _kv8_rows(cache, q, H, "q")
+    if out is None:
+        out = _empty((total, H, cache.d), q.dtype, q.device, stream)
+    elif out.dtype != q.dtype or out.shape[0] != total:
+        raise ValueError(f"out: {q.dtype} [{total}][{H}][{cache.d}] is wanted")
+    op, ot, oh = _kv8_rows(cache, out, H, "out")
+    if want_lse and lse is None:
+        lse = _empty((total, H), torch.float32, q.device, stream)
+    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (total, H) or not lse.is_contiguous() or lse.device != cache.device):
+        raise ValueError(f"lse: float32 [{total}][{H}] contiguous on {cache.device} is wanted")
+    workspace = _kv8_workspace(cache, max_q * G, workspace, stream)
+    if scale is None:
+        scale = 1.0 / float(np.sqrt(cache.d))
+    rc = lib().eosq_kv8_attend(ctx._h, cache._address, layer, qp, _any_dtype_code(q), total, qt, qh, _kv8_list(cache, seqs, None, "seqs"),
+                               _kv8_list(cache, cu, n + 1, "cu"), n, max_q, G, scale, int(causal), window, op, ot, oh,
+                               None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+    _check(rc, "eosq_kv8_attend", ctx)
+    return out if lse is None else (out, lse)
+
+
+def eosq_kv8_fork(ctx: Context, cache: Kv8Cache, src, dst, workspace=None, stream=None) -> None:
+    """Sequence dst[i], empty before, becomes a copy of sequence src[i]; they share whole pages."""
+    n = src.shape[0]
+    workspace = _kv8_workspace(cache, 0, workspace, stream)
+    rc = lib().eosq_kv8_fork(ctx._h, cache._address, _kv8_list(cache, src, None, "src"), _kv8_list(cache, dst, n, "dst"), n, workspace.data_ptr(),
+                             workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+    _check(rc, "eosq_kv8_fork", ctx)
+
+
+def eosq_kv8_free(ctx: Context, cache: Kv8Cache, seqs, stream=None) -> None:
+    rc = lib().eosq_kv8_free(ctx._h, cache._address, _kv8_list(cache, seqs, None, "seqs"), seqs.shape[0], _stream_ptr(stream))
+    _check(rc, "eosq_kv8_free", ctx)
+
+
+def eosq_kv8_compact(ctx: Context, cache: Kv8Cache, remap=None, workspace=None, stream=None):
+    """Moves the used pages to the front of the pool.  Returns where each page went, -1 for one that was free."""
+    import torch
+    if remap is None:
+        remap = _empty(cache.num_pages, torch.int32, cache.device, stream)
+    workspace = _kv8_workspace(cache, 0, workspace, stream)
+    rc = lib().eosq_kv8_compact(ctx._h, cache._address, _kv8_list(cache, remap, cache.num_pages, "remap"), workspace.data_ptr(),
+                                workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+    _check(rc, "eosq_kv8_compact", ctx)
+    return remap
+
+
+def eosq_kv8_copy_pages(ctx: Context, from_cache: Kv8Cache, to_cache: Kv8Cache, src_pages, dst_pages, stream=None) -> None:
+    """Pages src_pages[i] of one cache to dst_pages[i] of another of the same geometry (or of itself)."""
+    n = src_pages.shape[0]
+    if from_cache.device != to_cache.device:
+        raise ValueError("the caches are on different devices")
+    rc = lib().eosq_kv8_copy_pages(ctx._h, from_cache._address, to_cache._address, _kv8_list(from_cache, src_pages, None, "src_pages"),
+                                   _kv8_list(from_cache, dst_pages, n, "dst_pages"), n, _stream_ptr(stream))
+    _check(rc, "eosq_kv8_copy_pages", ctx)
+
+
+def eosq_kv8_check(ctx: Context, cache: Kv8Cache, stream=None) -> int:
+    """The EOSQ_KV8_* flags that calls on this cache have raised, which are then cleared (synchronises the stream)."""
+    flags = ctypes.c_uint32(0)
+    rc = lib().eosq_kv8_check(ctx._h, cache._address, ctypes.byref(flags), _stream_ptr(stream))
+    if rc not in (EOSQ_OK, EOSQ_WARN_BLOCK_STATUS):
+        _check(rc, "eosq_kv8_check", ctx)
+    return int(flags.value)

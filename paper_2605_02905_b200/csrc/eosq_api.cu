@@ -25,6 +25,34 @@ bool eosq::ensure_dynamic_smem(const void *kernel, size_t bytes) {
     return true;
 }
 
+// The context's buffers, constants and error word live on the device it was created on: every
+// device entry point refuses to run with another device current.
+bool eosq::on_ctx_device(eosq_ctx *ctx) {
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev != ctx->device) {
+        ctx->last_error = "the current CUDA device is not the one this context was created on";
+        return false;
+    }
+    return true;
+}
+
+bool eosq::record_cuda(eosq_ctx *ctx, cudaError_t err, const char *what) {
+    if (err == cudaSuccess) return false;
+    if (ctx) ctx->last_error = std::string(what) + ": " + cudaGetErrorString(err);
+    return true;
+}
+
+cudaEvent_t eosq::take_event(eosq_ctx *ctx) {
+    if (!ctx->free_events.empty()) {
+        cudaEvent_t e = ctx->free_events.back();
+        ctx->free_events.pop_back();
+        return e;
+    }
+    cudaEvent_t e = nullptr;
+    cudaEventCreate(&e);
+    return e;
+}
+
 int eosq::get_codebook(eosq_ctx *ctx, int d, int bits, Codebook *cb) {
     Codebook &own = ctx->codebooks[bits];
     if (own.bits != bits) {
@@ -40,23 +68,6 @@ int eosq::get_codebook(eosq_ctx *ctx, int d, int bits, Codebook *cb) {
 }
 
 namespace {
-
-// The context's buffers, constants and error word live on the device it was created on: every
-// device entry point refuses to run with another device current.
-bool on_ctx_device(eosq_ctx *ctx) {
-    int dev = -1;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev != ctx->device) {
-        ctx->last_error = "the current CUDA device is not the one this context was created on";
-        return false;
-    }
-    return true;
-}
-
-bool record_cuda(eosq_ctx *ctx, cudaError_t err, const char *what) {
-    if (err == cudaSuccess) return false;
-    if (ctx) ctx->last_error = std::string(what) + ": " + cudaGetErrorString(err);
-    return true;
-}
 
 int check_shape(int n, int d, int bits) {
     if (d != D || bits < 1 || bits > 4 || n < d || n > NMAX || (n % 8) != 0) return EOSQ_ERR_UNSUPPORTED;
@@ -110,33 +121,6 @@ eosq_cache_t shifted(const eosq_cache_t &c, int64_t b0, int n, int bits) {
     if (o.vr32) o.vr32 += b0 * RMAX * D;
     if (o.coef) o.coef += b0 * RMAX;
     return o;
-}
-
-cudaEvent_t take_event(eosq_ctx *ctx) {
-    if (!ctx->free_events.empty()) {
-        cudaEvent_t e = ctx->free_events.back();
-        ctx->free_events.pop_back();
-        return e;
-    }
-    cudaEvent_t e = nullptr;
-    cudaEventCreate(&e);
-    return e;
-}
-
-// Runs `launch` (which enqueues one kernel on `s`; the score path adds its extra ones itself), counting it and, when profiling is
-// on, bracketing it with events.
-template <typename F>
-void run_stage(eosq_ctx *ctx, int stage, cudaStream_t s, F &&launch) {
-    if ((ctx->profile_mask >> stage) & 1u) {
-        eosq_ctx::Timed t{stage, take_event(ctx), take_event(ctx)};
-        cudaEventRecord(t.start, s);
-        launch();
-        cudaEventRecord(t.stop, s);
-        ctx->timed.push_back(t);
-    } else {
-        launch();
-    }
-    ctx->launches += 1;
 }
 
 bool cache_required_ok(const eosq_cache_t *c) {

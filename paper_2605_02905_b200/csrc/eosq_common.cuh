@@ -156,6 +156,27 @@ struct eosq_ctx {
 
 namespace eosq {
 
+// ---- host helpers of the entry points (eosq_api.cu) ---------------------------------------
+bool on_ctx_device(eosq_ctx *ctx);
+bool record_cuda(eosq_ctx *ctx, cudaError_t err, const char *what);   // true: an error, whose text the context keeps
+cudaEvent_t take_event(eosq_ctx *ctx);
+
+// Runs `launch` (which enqueues one kernel on `s`; the score path adds its extra ones itself), counting it and, when profiling is
+// on, bracketing it with events.
+template <typename F>
+void run_stage(eosq_ctx *ctx, int stage, cudaStream_t s, F &&launch) {
+    if ((ctx->profile_mask >> stage) & 1u) {
+        eosq_ctx::Timed t{stage, take_event(ctx), take_event(ctx)};
+        cudaEventRecord(t.start, s);
+        launch();
+        cudaEventRecord(t.stop, s);
+        ctx->timed.push_back(t);
+    } else {
+        launch();
+    }
+    ctx->launches += 1;
+}
+
 // The launch sequence of the encode path for blocks [b0, b0 + nb) of `blocks` (implemented with
 // the C entry points; shared by eosq_encode and eosq_encode_static).
 int encode_chunk(eosq_ctx *ctx, const void *blocks, int in_dtype, int64_t b0, int64_t nb, int n, int bits,

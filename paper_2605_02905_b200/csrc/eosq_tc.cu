@@ -75,6 +75,19 @@ bool make_factor_tensor_map(const void *P, int64_t nb, int n, int rows, CUtensor
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Tensor map over the 8-bit cache's codes: [rows][d] bytes, boxes of box_rows rows, swizzled over a row's width.
+bool make_code_tensor_map(const void *codes, long long rows, int d, int box_rows, CUtensorMap *out) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(d)};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(d), static_cast<cuuint32_t>(box_rows)};
+    const cuuint32_t estr[2] = {1, 1};
+    return fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(codes), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // ------------------------------------------------------------------------------------------
 // Gram matrix.  Persistent CTAs: warp 0 loads token tiles by TMA into a ring of
 // stages, warp 1 issues the MMAs, ten warps from 4 on add finished partial sums into fp64 registers.
