@@ -3,6 +3,7 @@
 #pragma once
 
 #include <cuda.h>
+#include <cuda_bf16.h>
 #include <cuda_fp8.h>
 
 #include "eosq_common.cuh"
@@ -76,6 +77,11 @@ __device__ __forceinline__ Kv8Seq kv8_seq(const Kv8 &c, const int32_t *seqs, con
 }
 
 // ---- attention ----------------------------------------------------------------------------------
+// A row tile that begins in one CTA and ends in another (last_cta; -1: there is none).
+struct Kv8Cut {
+    int last_cta, q0, m, r, h, unused[3];
+};
+constexpr int KV8_MAX_CTAS = 320;
 struct Kv8Attend {
     Kv8 c;
     const int32_t *seqs, *cu;
@@ -86,7 +92,7 @@ struct Kv8Attend {
     float *lse;
     long long q_tok, q_head, o_tok, o_head;   // strides in elements
     float scale_log2;                          // scale * log2(e)
-    int32_t *first_unit;                       // [n + 1] scratch: units before each entry
+    Kv8Cut *cuts;                       // [KV8_MAX_CTAS] scratch: row tiles that go on in the next CTA
     float *part;                               // scratch: partial results, two slots per CTA
     int *err;
 };
@@ -117,6 +123,57 @@ __device__ __forceinline__ int unit_of(int units, int cta, int ctas) { return st
 __device__ __forceinline__ int cta_of(int units, int unit, int ctas) {
     return static_cast<int>(((static_cast<long long>(unit) + 1) * ctas - 1) / units);
 }
+// The row tiles and heads of a run of units, one after another; the same in every thread of a warp.
+template <typename T>
+struct Kv8Walk {
+    const Kv8Attend &a;
+    int i, at, left;                          // entry; units of it that come before; units to go
+    Kv8Seq s;
+    int row_tiles, r, h, tile0, tiles, from, take;   // now: row tile, head, its key tiles [tile0, tile0 + tiles), of which `take` from `from` on are the run's
+    bool fresh;
+    __device__ __forceinline__ Kv8Walk(const Kv8Attend &a_, int entry, int skip, int units) : a(a_), i(entry), at(skip), left(units), r(0), h(0), tiles(1), fresh(true) {
+        if (left > 0) enter();
+    }
+    __device__ __forceinline__ void enter() {
+        s = kv8_seq(a.c, a.seqs, a.cu, i, a.total, a.max_q);
+        row_tiles = (s.m > 0) ? T::row_tiles(a, s) : 0;
+        r = 0;
+    }
+    __device__ __forceinline__ bool next() {
+        if (left <= 0) return false;
+        from = 0;
+        if (!fresh && ++h < a.c.heads) {
+            take = min(tiles, left);
+            left -= take;
+            return true;
+        }
+        if (!fresh) ++r;
+        fresh = false;
+        h = 0;
+        while (true) {
+            if (r >= row_tiles) {
+                if (++i >= a.n) {   // (the units say that there is more; unless memory changes under the call)
+                    left = 0;
+                    return false;
+                }
+                enter();
+                continue;
+            }
+            tiles = T::key_tiles(a, s, r, tile0);
+            if (at < tiles * a.c.heads) break;
+            at -= tiles * a.c.heads;
+            ++r;
+        }
+        h = at / tiles;
+        from = at - h * tiles;
+        at = 0;
+        take = min(tiles - from, left);
+        left -= take;
+        return true;
+    }
+    // -1: the whole row tile is in the run, else the slot of its partial result: 1 for the run's last, 0 for one that began before.
+    __device__ __forceinline__ int slot() const { return (take == tiles) ? -1 : (from == 0 ? 1 : 0); }
+};
 // Scores are base-2 logarithms; a weight is 2^(x - m + KV8_SHIFT), m being a running maximum that is only moved when a score passes
 // it by more than KV8_SLACK.  So weights are at most 2^14, inside fp16, and those of fp16's smallest normal numbers are 2^-20 of
 // the largest when m is exact.  x contains log2 of the page's value scale, so that the product with the codes of the values needs no
@@ -132,6 +189,163 @@ __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
+// Exclusive prefix sums of units[0 .. n) in place, by one warp; the total.
+__device__ __forceinline__ int warp_prefix(int *units, int n) {
+    const int lane = threadIdx.x & 31;
+    int total = 0;
+    for (int base = 0; base < n; base += 32) {
+        const int v = (base + lane < n) ? units[base + lane] : 0;
+        int x = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+        }
+        if (base + lane < n) units[base + lane] = total + x - v;
+        total += __shfl_sync(0xffffffffu, x, 31);
+    }
+    return total;
+}
+
+template <bool BF16, int N>
+__device__ __forceinline__ void store_row(void *p, const float (&v)[N]) {
+    uint32_t w[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        if constexpr (BF16) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t *>(&b);
+        } else {
+            w[i] = half2_bits(v[2 * i], v[2 * i + 1]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N / 8; ++i) reinterpret_cast<uint4 *>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+}
+
+// A CTA's run of units: first entry, units of it that come before, [u0, u1) of `total`, the runs that there are.
+struct Kv8Run {
+    int entry, skip, u0, u1, total, ctas;
+};
+// Every thread of the CTA (of THREADS) takes part; `units` is shared memory for every entry's units, which may be used otherwise once this has returned.
+template <typename T, int THREADS>
+__device__ __forceinline__ Kv8Run kv8_run(const Kv8Attend &a, int *units) {
+    __shared__ int total_units;
+    const int tid = threadIdx.x;
+    for (int i = tid; i < a.n; i += THREADS) {
+        const Kv8Seq s = kv8_seq(a.c, a.seqs, a.cu, i, a.total, a.max_q);
+        int u = 0;
+        if (s.m > 0) {
+            const int tiles = T::row_tiles(a, s);
+            int first;
+            for (int r = 0; r < tiles; ++r) u += T::key_tiles(a, s, r, first);
+        }
+        units[i] = u * a.c.heads;
+    }
+    __syncthreads();
+    if (tid < 32) {
+        const int t = warp_prefix(units, a.n);
+        if (tid == 0) total_units = t;
+    }
+    __syncthreads();
+    Kv8Run run{0, 0, 0, 0, total_units, min(static_cast<int>(gridDim.x), total_units)};
+    const int cta = blockIdx.x;
+    if (cta < run.ctas) {
+        run.u0 = unit_of(run.total, cta, run.ctas);
+        run.u1 = unit_of(run.total, cta + 1, run.ctas);
+        int lo = 0, hi = a.n;   // the last entry that begins at or before u0 (those behind with the same beginning have no units)
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (units[mid] <= run.u0) lo = mid;
+            else hi = mid;
+        }
+        run.entry = lo;
+        run.skip = run.u0 - units[lo];
+    } else if (tid == 0) {
+        a.cuts[cta].last_cta = -1;
+    }
+    __syncthreads();
+    return run;
+}
+
+// log sum exp of a row from its maximum and the sum of its weights (both as the kernels hold them): -infinity for a row that saw nothing, whose maximum is
+// -infinity and whose sum is 0; NaN for one with a NaN among its scores, whose sum is that.
+__device__ __forceinline__ float row_lse(float m, float l) {
+    return (m - KV8_SHIFT + log2f(l)) * 0.6931471805599453f;
+}
+
+// Partial results: [slots][ROWS][d] sums, then [slots][ROWS] maxima, then sums of weights.
+template <int RT>
+struct Kv8Parts {
+    float *o, *m, *l;
+    __device__ __forceinline__ Kv8Parts(const Kv8Attend &a, int ctas) {
+        const size_t rows = static_cast<size_t>(2) * ctas * RT;
+        o = a.part;
+        m = o + (rows << a.c.d_shift);
+        l = m + rows;
+    }
+};
+
+// What a CTA says about its last row tile: whether it goes on behind the run [.., u1) of `ctas` runs.
+template <typename T>
+__device__ __forceinline__ void kv8_cut(const Kv8Walk<T> &w, int total, int u1, int ctas) {
+    Kv8Cut cut{-1, w.s.q0, w.s.m, w.r, w.h, {0, 0, 0}};
+    if (w.from == 0 && w.take < w.tiles) cut.last_cta = cta_of(total, u1 - w.take + w.tiles - 1, ctas);
+    w.a.cuts[blockIdx.x] = cut;
+}
+
+// Row tiles that several CTAs worked on: their partial results under one maximum, in the order of the keys.  A CTA of this kernel per 16 rows and
+// CTA of the other, which a row tile may begin in and not end.
+template <int RT, int DIM, bool BF16>
+__global__ void __launch_bounds__(128) kv8_join_kernel(const Kv8Attend a, int ctas) {
+    pdl_wait();
+    constexpr int PER = RT / 16;
+    const int ca = blockIdx.x / PER, row0 = (blockIdx.x % PER) * 16;
+    const Kv8Cut cut = a.cuts[ca];
+    const int rows = cut.m * a.G;
+    if (cut.last_cta < 0 || cut.r * RT + row0 >= rows) return;
+    const Kv8Parts<RT> parts(a, ctas);
+    constexpr int PART = 8, LANES = DIM / PART;   // threads per row
+    for (int row = row0 + threadIdx.x / LANES; row < row0 + 16; row += 128 / LANES) {
+        const int at = cut.r * RT + row, part = threadIdx.x % LANES;
+        if (at >= rows) break;
+        float top = -INFINITY;
+        for (int k = ca; k <= cut.last_cta; ++k) top = fmaxf(top, parts.m[static_cast<size_t>(2 * k + (k == ca)) * RT + row]);
+        float l = 0.0f, v[PART];
+#pragma unroll
+        for (int e = 0; e < PART; ++e) v[e] = 0.0f;
+        for (int k = ca; k <= cut.last_cta; ++k) {
+            const size_t pr = static_cast<size_t>(2 * k + (k == ca)) * RT + row;
+            const float mk = parts.m[pr], f = (mk == -INFINITY) ? 0.0f : exp2_fast(mk - top);
+            l = fmaf(parts.l[pr], f, l);
+            const float4 x = *reinterpret_cast<const float4 *>(parts.o + pr * DIM + part * PART);
+            const float4 y = *reinterpret_cast<const float4 *>(parts.o + pr * DIM + part * PART + 4);
+            v[0] = fmaf(x.x, f, v[0]); v[1] = fmaf(x.y, f, v[1]); v[2] = fmaf(x.z, f, v[2]); v[3] = fmaf(x.w, f, v[3]);
+            v[4] = fmaf(y.x, f, v[4]); v[5] = fmaf(y.y, f, v[5]); v[6] = fmaf(y.z, f, v[6]); v[7] = fmaf(y.w, f, v[7]);
+        }
+        const float inv = (top == -INFINITY) ? 0.0f : 1.0f / l;
+#pragma unroll
+        for (int e = 0; e < PART; ++e) v[e] *= inv;
+        const long long tq = cut.q0 + at / a.G;
+        const int hq = cut.h * a.G + at % a.G;
+        store_row<BF16, PART>(static_cast<__half *>(a.out) + tq * a.o_tok + hq * a.o_head + part * PART, v);
+        if (a.lse && part == 0) a.lse[tq * (a.c.heads * a.G) + hq] = row_lse(top, l);
+    }
+}
+
+template <int RT>
+void launch_join(const Kv8Attend &a, int dtype, int ctas, cudaStream_t s) {
+    const dim3 grid(static_cast<unsigned>(ctas) * (RT / 16));
+    const bool bf = dtype == EOSQ_BF16;
+    if (a.c.d_shift == 7) {
+        if (bf) launch_dependent(kv8_join_kernel<RT, 128, true>, grid, 128, 0, s, a, ctas);
+        else launch_dependent(kv8_join_kernel<RT, 128, false>, grid, 128, 0, s, a, ctas);
+    } else {
+        if (bf) launch_dependent(kv8_join_kernel<RT, 64, true>, grid, 128, 0, s, a, ctas);
+        else launch_dependent(kv8_join_kernel<RT, 64, false>, grid, 128, 0, s, a, ctas);
+    }
+}
+
 // ---- launchers ------------------------------------------------------------------------------------
 void launch_kv8_store(const Kv8 &c, int fmt, const void *const (&x)[2], int dtype, long long total, const long long (&tok)[2],
                       const long long (&head)[2], const int32_t *seqs, const int32_t *first, const int32_t *cu, int n, int max_new, cudaStream_t s);
@@ -144,9 +358,15 @@ void launch_kv8_compact_move(const Kv8 &c, const int32_t *remap, const int32_t *
 void launch_kv8_copy(const Kv8 &from, const Kv8 &to, const int32_t *src, const int32_t *dst, int n, cudaStream_t s);
 // Attention: scratch for a call's partial results, the kernel (EOSQ_OK, EOSQ_ERR_UNSUPPORTED or EOSQ_ERR_CUDA; nothing enqueued unless OK), and the one that
 // joins what CTAs share between them.
-size_t kv8_attend_scratch(int query_rows, int d);
-int launch_kv8_attend(const Kv8Attend &a, int fmt, int dtype, int sm_count, cudaStream_t s);
-void launch_kv8_join(const Kv8Attend &a, int dtype, int sm_count, cudaStream_t s);
+size_t kv8_rows_scratch(int d);
+size_t kv8_tiles_scratch(int d);
+int launch_kv8_rows(const Kv8Attend &a, int fmt, int dtype, int sm_count, cudaStream_t s);
+int launch_kv8_tiles(const Kv8Attend &a, int fmt, int dtype, int sm_count, cudaStream_t s);
+void launch_kv8_rows_join(const Kv8Attend &a, int dtype, int sm_count, cudaStream_t s);
+void launch_kv8_tiles_join(const Kv8Attend &a, int dtype, int sm_count, cudaStream_t s);
+// Up to so many query rows per KV head and entry go through the kernel for few rows (eosq_kv8_attend.cu), more through the one that works on
+// tiles of 256 rows (eosq_kv8_attend_tc.cu).
+constexpr int KV8_FEW_ROWS = 16;
 // Tensor map over the codes of a layer's keys or values, [rows][d] bytes, in boxes of box_rows rows with a swizzle as wide as a row (eosq_tc.cu).
 bool make_code_tensor_map(const void *codes, long long rows, int d, int box_rows, CUtensorMap *out);
 

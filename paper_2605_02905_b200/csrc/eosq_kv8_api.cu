@@ -73,7 +73,8 @@ int entry(F &&f) {
 size_t pages_scratch(const eosq_kv8_t *c) {
     return std::max(sizeof(int2) * static_cast<size_t>(c->max_seqs), sizeof(int32_t) * (64 + static_cast<size_t>(c->num_pages)));
 }
-size_t units_scratch() { return align_up(sizeof(int32_t) * (EOSQ_KV8_MAX_SEQS + 1), 256); }
+size_t kv8_attend_scratch(int64_t rows, int d) { return rows <= KV8_FEW_ROWS ? kv8_rows_scratch(d) : kv8_tiles_scratch(d); }
+size_t cuts_scratch() { return align_up(sizeof(Kv8Cut) * KV8_MAX_CTAS, 256); }
 
 int set_up_failed(eosq_ctx *ctx, const char *what) {
     ctx->last_error = what;
@@ -85,7 +86,7 @@ int set_up_failed(eosq_ctx *ctx, const char *what) {
 extern "C" size_t eosq_kv8_workspace_bytes(const eosq_kv8_t *cache, int query_rows) {
     if (query_rows < 0 || view_of(cache, 0, nullptr) == EOSQ_ERR_UNSUPPORTED || !cache || cache->max_seqs <= 0 || cache->num_pages <= 0) return 0;
     size_t bytes = pages_scratch(cache);
-    if (query_rows > 0) bytes = std::max(bytes, units_scratch() + kv8_attend_scratch(query_rows, cache->d));
+    if (query_rows > 0) bytes = std::max(bytes, cuts_scratch() + kv8_attend_scratch(query_rows, cache->d));
     return align_up(bytes, 256);
 }
 
@@ -148,7 +149,7 @@ extern "C" int eosq_kv8_attend(eosq_ctx *ctx, const eosq_kv8_t *cache, int layer
             misaligned(lse, 3) || !workspace || misaligned(workspace, 255))
             return EOSQ_ERR_INVALID_ARG;
         const int most = static_cast<int>(std::min<int64_t>(max_q, total));
-        if (workspace_bytes < units_scratch() + kv8_attend_scratch(most * G, cache->d)) return EOSQ_ERR_BUFFER_TOO_SMALL;
+        if (workspace_bytes < cuts_scratch() + kv8_attend_scratch(most * G, cache->d)) return EOSQ_ERR_BUFFER_TOO_SMALL;
         if (!on_ctx_device(ctx)) return EOSQ_ERR_INVALID_ARG;
         a.seqs = seqs;
         a.cu = cu;
@@ -167,15 +168,20 @@ extern "C" int eosq_kv8_attend(eosq_ctx *ctx, const eosq_kv8_t *cache, int layer
         a.o_head = out_head_stride;
         a.scale_log2 = scale * 1.4426950408889634f;
         char *p = static_cast<char *>(workspace);
-        a.first_unit = reinterpret_cast<int32_t *>(p);
-        a.part = reinterpret_cast<float *>(p + units_scratch());
+        a.cuts = reinterpret_cast<Kv8Cut *>(p);
+        a.part = reinterpret_cast<float *>(p + cuts_scratch());
         a.err = ctx->dev_err;
         cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
         int why = 0;
-        run_stage(ctx, ST_OTHER, s, [&] { why = launch_kv8_attend(a, cache->format, dtype, ctx->sm_count, s); });
-        if (why == EOSQ_ERR_UNSUPPORTED) return why;
+        const bool few = most * G <= KV8_FEW_ROWS;
+        run_stage(ctx, ST_OTHER, s, [&] {
+            why = few ? launch_kv8_rows(a, cache->format, dtype, ctx->sm_count, s) : launch_kv8_tiles(a, cache->format, dtype, ctx->sm_count, s);
+        });
         if (why) return set_up_failed(ctx, "eosq_kv8_attend: tensor map or launch set-up failed");
-        run_stage(ctx, ST_OTHER, s, [&] { launch_kv8_join(a, dtype, ctx->sm_count, s); });
+        run_stage(ctx, ST_OTHER, s, [&] {
+            if (few) launch_kv8_rows_join(a, dtype, ctx->sm_count, s);
+            else launch_kv8_tiles_join(a, dtype, ctx->sm_count, s);
+        });
         return record_cuda(ctx, cudaGetLastError(), "eosq_kv8_attend launch") ? EOSQ_ERR_CUDA : EOSQ_OK;
     });
 }

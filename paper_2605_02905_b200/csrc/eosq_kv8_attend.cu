@@ -17,7 +17,7 @@ namespace {
 // warps work on 16 tokens of every tile each, with statistics and sums of their own, which meet at the end of a row tile.
 constexpr int ROWS = 16, KEYS = 64, GROUP = 16;         // query rows; tokens of a tile; tokens of a warp's share, all in one page
 constexpr int WORKERS = KEYS / GROUP, THREADS = 32 * (WORKERS + 1);
-constexpr int STAGES = 4, CTAS_PER_SM = 2, MAX_CTAS = 320;
+constexpr int STAGES = 4, CTAS_PER_SM = 2;
 using Tiles = Kv8Tiles<ROWS, KEYS>;
 
 struct TileInfo {
@@ -36,24 +36,6 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4],
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-// Exclusive prefix sums of units[0 .. n) in place, by one warp; the total.
-__device__ __forceinline__ int warp_prefix(int *units, int n) {
-    const int lane = threadIdx.x & 31;
-    int total = 0;
-    for (int base = 0; base < n; base += 32) {
-        const int v = (base + lane < n) ? units[base + lane] : 0;
-        int x = v;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, x, o);
-            if (lane >= o) x += y;
-        }
-        if (base + lane < n) units[base + lane] = total + x - v;
-        total += __shfl_sync(0xffffffffu, x, 31);
-    }
-    return total;
 }
 
 // NQ query values of a row, as fp16.  bf16 values are first multiplied by a power of two that brings the row's largest to 2^14 .. 2^15:
@@ -86,53 +68,18 @@ __device__ __forceinline__ float query_row(const void *p, uint32_t (&v)[NQ / 2],
     return __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
 }
 
-template <bool BF16, int N>
-__device__ __forceinline__ void store_row(void *p, const float (&v)[N]) {
-    uint32_t w[N / 2];
-#pragma unroll
-    for (int i = 0; i < N / 2; ++i) {
-        if constexpr (BF16) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t *>(&b);
-        } else {
-            w[i] = half2_bits(v[2 * i], v[2 * i + 1]);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < N / 8; ++i) reinterpret_cast<uint4 *>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-}
-
-// log sum exp of a row from its maximum and the sum of its weights (both as the kernels hold them); -infinity for a row that saw nothing.
-__device__ __forceinline__ float row_lse(float m, float l) {
-    return (m == -INFINITY) ? -INFINITY : (m - KV8_SHIFT + log2f(l)) * 0.6931471805599453f;
-}
-
-// Partial results: [slots][ROWS][d] sums, then [slots][ROWS] maxima, then sums of weights.
-template <int RT>
-struct Parts {
-    float *o, *m, *l;
-    __device__ __forceinline__ Parts(const Kv8Attend &a, int ctas) {
-        const size_t rows = static_cast<size_t>(2) * ctas * RT;
-        o = a.part;
-        m = o + (rows << a.c.d_shift);
-        l = m + rows;
-    }
-};
-
 template <int DIM, int FMT, bool BF16>
 __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
                                                                           const Kv8Attend a) {
     extern __shared__ uint8_t rows_smem[];
     __shared__ __align__(8) uint64_t full_bar[STAGES], empty_bar[STAGES], join_bar;
     __shared__ TileInfo info[STAGES];
-    __shared__ int total_units;
     __shared__ volatile int abort_flag;
     __shared__ uint32_t fills[STAGES];
     __shared__ float top_s[WORKERS][ROWS], sum_s[WORKERS][ROWS];
     constexpr int TILE = KEYS * DIM;   // bytes of a tile's keys, or values
     uint8_t *stages = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(rows_smem) + 1023) & ~static_cast<uintptr_t>(1023));
     float *sums = reinterpret_cast<float *>(stages + STAGES * TILE * 2);
-    int *units = reinterpret_cast<int *>(sums);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const Kv8 &c = a.c;
     if (tid == 0) {
@@ -148,121 +95,73 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
         fence_mbar_init();
     }
     pdl_wait();
-    for (int i = tid; i < a.n; i += THREADS) {
-        const Kv8Seq s = kv8_seq(c, a.seqs, a.cu, i, a.total, a.max_q);
-        int u = 0;
-        if (s.m > 0) {
-            const int tiles = Tiles::row_tiles(a, s);
-            int first;
-            for (int r = 0; r < tiles; ++r) u += Tiles::key_tiles(a, s, r, first);
-        }
-        units[i] = u * c.heads;
-    }
-    __syncthreads();
-    if (warp == 0) {
-        const int t = warp_prefix(units, a.n);
-        if (lane == 0) total_units = t;
-        if (blockIdx.x == 0) {
-            for (int i = lane; i < a.n; i += 32) a.first_unit[i] = units[i];
-            if (lane == 0) a.first_unit[a.n] = t;
-        }
-    }
-    __syncthreads();
-    const int total = total_units, ctas = min(static_cast<int>(gridDim.x), total), cta = blockIdx.x;
-    const int u0 = (cta < ctas) ? unit_of(total, cta, ctas) : 0, u1 = (cta < ctas) ? unit_of(total, cta + 1, ctas) : 0;
-    int i = 0;
-    if (u0 < u1) {   // the entry of the first unit: the last one that begins at or before it (those behind with the same beginning have no units)
-        int lo = 0, hi = a.n;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (units[mid] <= u0) lo = mid;
-            else hi = mid;
-        }
-        i = lo;
-    }
-    const int skip = (u0 < u1) ? u0 - units[i] : 0;
-    __syncthreads();   // the units' place is the sums' from here on
+    const Kv8Run run = kv8_run<Tiles, THREADS>(a, reinterpret_cast<int *>(sums));
 
     if (warp == WORKERS) {
         uint32_t it = 0;
         bool ok = true;
-        int left = u1 - u0, at = skip;   // units to go; units of the entry's rest that come before
-        for (; left > 0 && ok; ++i) {
-            const Kv8Seq s = kv8_seq(c, a.seqs, a.cu, i, a.total, a.max_q);
-            const int row_tiles = (s.m > 0) ? Tiles::row_tiles(a, s) : 0;
-            const int32_t *pages = c.table + static_cast<size_t>(s.row < 0 ? 0 : s.row) * c.max_pages;
-            for (int r = 0; r < row_tiles && left > 0 && ok; ++r) {
-                int tile0;
-                const int tiles = Tiles::key_tiles(a, s, r, tile0);
-                if (at >= tiles * c.heads) {
-                    at -= tiles * c.heads;
-                    continue;
-                }
-                int lo, hi;
-                Tiles::span(a, s, r * ROWS / a.G, min(s.m - 1, (r * ROWS + ROWS - 1) / a.G), lo, hi);
-                for (int h = at / tiles; h < c.heads && left > 0 && ok; ++h) {
-                    const int from = (h == at / tiles) ? at % tiles : 0, take = min(tiles - from, left);
-                    const int slot = (from == 0 && take == tiles) ? -1 : (from == 0 ? 1 : 0);
-                    const int box = min(c.page_size(), KEYS);
-                    for (int t = 0; t < take && ok; ++t, ++it) {
-                        const int st = it % STAGES;
-                        const int tok0 = (tile0 + from + t) * KEYS;
-                        // the page of each 16 tokens, its scales; a box is what one page gives to a tile
-                        float ks = 0.0f, vs = 1.0f, vlog = -INFINITY;
-                        int page = -1;
-                        const int tok = tok0 + lane * GROUP, box0 = tok & ~(box - 1);
-                        if (lane < WORKERS && box0 < hi && box0 + box > lo) {
-                            page = pages[tok >> c.ps_shift];
-                            if (page < 0 || page >= c.num_pages) {
-                                raise(c, EOSQ_KV8_BAD_PAGE);
-                                page = -1;
-                            } else {
-                                const size_t at_scale = static_cast<size_t>(page) * c.heads + h;
-                                ks = c.scale[0][at_scale] * (Kv8Unit<FMT>::value * a.scale_log2);
-                                vs = fminf(fmaxf(c.scale[1][at_scale], KV8_SCALE_MIN), KV8_SCALE_MAX) * Kv8Unit<FMT>::value;
-                                vlog = log2f(vs);
-                            }
-                        }
-                        ok = mbar_wait_warp(&empty_bar[st], ((it / STAGES) & 1u) ^ 1u, &abort_flag);
-                        if (!ok) break;
-                        const bool leader = page >= 0 && (tok & (box - 1)) == 0;
-                        const unsigned boxes = __popc(__ballot_sync(0xffffffffu, leader));
-                        if (lane < WORKERS) {
-                            info[st].ks[lane] = ks;
-                            info[st].vlog[lane] = vlog;
-                            info[st].vinv[lane] = 1.0f / vs;
-                        }
-                        if (lane == 0) {
-                            info[st].first = t == 0;
-                            info[st].last = t == take - 1;
-                            info[st].tok0 = tok0;
-                            info[st].q0 = s.q0;
-                            info[st].len = s.len;
-                            info[st].m = s.m;
-                            info[st].r = r;
-                            info[st].h = h;
-                            info[st].slot = slot;
-                        }
-                        __syncwarp();
-                        if (lane == 0) {
-                            mbar_arrive_expect_tx(&full_bar[st], boxes * box * DIM * 2);
-                            fills[st] += 1;
-                        }
-                        __syncwarp();
-                        if (leader) {
-                            uint8_t *dst = stages + st * TILE * 2 + (tok - tok0) * DIM;
-                            const int row = ((page * c.heads + h) << c.ps_shift) + (tok & (c.page_size() - 1));
-                            tma_load_2d(dst, &kmap, &full_bar[st], 0, row);
-                            tma_load_2d(dst + TILE, &vmap, &full_bar[st], 0, row);
-                        }
-                        __syncwarp();
+        Kv8Walk<Tiles> w(a, run.entry, run.skip, run.u1 - run.u0);
+        const int box = min(c.page_size(), KEYS);   // what one page gives to a tile
+        while (ok && w.next()) {
+            const Kv8Seq &s = w.s;
+            const int32_t *pages = c.table + static_cast<size_t>(s.row) * c.max_pages;
+            int lo, hi;
+            Tiles::span(a, s, w.r * ROWS / a.G, min(s.m - 1, (w.r * ROWS + ROWS - 1) / a.G), lo, hi);
+            for (int t = 0; t < w.take; ++t, ++it) {
+                const int st = it % STAGES;
+                const int tok0 = (w.tile0 + w.from + t) * KEYS;
+                // the page of each 16 tokens, and its scales
+                float ks = 0.0f, vs = 1.0f, vlog = -INFINITY;
+                int page = -1;
+                const int tok = tok0 + lane * GROUP, box0 = tok & ~(box - 1);
+                if (lane < WORKERS && box0 < hi && box0 + box > lo) {
+                    page = pages[tok >> c.ps_shift];
+                    if (page < 0 || page >= c.num_pages) {
+                        raise(c, EOSQ_KV8_BAD_PAGE);
+                        page = -1;
+                    } else {
+                        const size_t slot = static_cast<size_t>(page) * c.heads + w.h;
+                        ks = c.scale[0][slot] * (Kv8Unit<FMT>::value * a.scale_log2);
+                        vs = fminf(fmaxf(c.scale[1][slot], KV8_SCALE_MIN), KV8_SCALE_MAX) * Kv8Unit<FMT>::value;
+                        vlog = log2f(vs);
                     }
-                    left -= take;
                 }
-                at = 0;
+                ok = mbar_wait_warp(&empty_bar[st], ((it / STAGES) & 1u) ^ 1u, &abort_flag);
+                if (!ok) break;
+                const bool leader = page >= 0 && (tok & (box - 1)) == 0;
+                const unsigned boxes = __popc(__ballot_sync(0xffffffffu, leader));
+                if (lane < WORKERS) {
+                    info[st].ks[lane] = ks;
+                    info[st].vlog[lane] = vlog;
+                    info[st].vinv[lane] = 1.0f / vs;
+                }
+                if (lane == 0) {
+                    info[st].first = t == 0;
+                    info[st].last = t == w.take - 1;
+                    info[st].tok0 = tok0;
+                    info[st].q0 = s.q0;
+                    info[st].len = s.len;
+                    info[st].m = s.m;
+                    info[st].r = w.r;
+                    info[st].h = w.h;
+                    info[st].slot = w.slot();
+                }
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive_expect_tx(&full_bar[st], boxes * box * DIM * 2);
+                    fills[st] += 1;
+                }
+                __syncwarp();
+                if (leader) {
+                    uint8_t *dst = stages + st * TILE * 2 + (tok - tok0) * DIM;
+                    const int row = ((page * c.heads + w.h) << c.ps_shift) + (tok & (c.page_size() - 1));
+                    tma_load_2d(dst, &kmap, &full_bar[st], 0, row);
+                    tma_load_2d(dst + TILE, &vmap, &full_bar[st], 0, row);
+                }
+                __syncwarp();
             }
-            if (row_tiles > 0) at = 0;
         }
+        if (lane == 0 && run.u0 < run.u1) kv8_cut(w, run.total, run.u1, run.ctas);
     } else {
         constexpr int STEPS = DIM / 16, WORDS = DIM / 32, OWN = DIM / 4;   // MMA steps over d; words of a token's values per lane; a lane's share of a row
         const int g = lane >> 2, q = lane & 3;                              // (g: row or token; q: which part of it)
@@ -271,7 +170,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
         int lo0 = 0, hi0 = 0, lo1 = 0, hi1 = 0, lo_all = 0, hi_all = 0, lo_max = 0, hi_min = 0;
         uint32_t joins = 0;
         bool ok = true;
-        for (uint32_t it = 0; it < static_cast<uint32_t>(u1 - u0); ++it) {
+        for (uint32_t it = 0; it < static_cast<uint32_t>(run.u1 - run.u0); ++it) {
             const int st = it % STAGES;
             ok = mbar_wait_warp(&full_bar[st], (it / STAGES) & 1u, &abort_flag);
             if (!ok) break;
@@ -490,7 +389,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
                     store_row<BF16, PART>(static_cast<__half *>(a.out) + tq * a.o_tok + hq * a.o_head + part * PART, v);
                     if (a.lse && part == 0) a.lse[tq * (c.heads * a.G) + hq] = row_lse(top, l);
                 } else {
-                    const Parts<ROWS> parts(a, gridDim.x);
+                    const Kv8Parts<ROWS> parts(a, gridDim.x);
                     const size_t pr = static_cast<size_t>(2 * blockIdx.x + slot) * ROWS + row;
 #pragma unroll
                     for (int k = 0; k < PART; k += 4)
@@ -514,54 +413,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
     }
 }
 
-// Row tiles that several CTAs worked on: their partial results under one maximum, in the order of the keys.  A CTA per row tile, head and entry.
-template <int RT, int KT, int DIM, bool BF16>
-__global__ void __launch_bounds__(128) kv8_join_kernel(const Kv8Attend a, int ctas, int most_tiles) {
-    using T = Kv8Tiles<RT, KT>;
-    pdl_wait();
-    const Kv8 &c = a.c;
-    const int h = blockIdx.x % c.heads, rest = blockIdx.x / c.heads, r = rest % most_tiles, i = rest / most_tiles;
-    const int total = a.first_unit[a.n];
-    int u = a.first_unit[i];
-    if (total == 0 || a.first_unit[i + 1] == u) return;
-    const Kv8Seq s = kv8_seq(c, a.seqs, a.cu, i, a.total, a.max_q);
-    if (s.m == 0 || r >= T::row_tiles(a, s)) return;
-    int first;
-    for (int k = 0; k < r; ++k) u += T::key_tiles(a, s, k, first) * c.heads;
-    const int tiles = T::key_tiles(a, s, r, first);
-    u += h * tiles;
-    const int working = min(ctas, total), ca = cta_of(total, u, working), cb = cta_of(total, u + tiles - 1, working);
-    if (ca == cb) return;   // written by that CTA
-    const Parts<RT> parts(a, ctas);
-    constexpr int PART = 8, LANES = DIM / PART;   // threads per row
-    for (int row = threadIdx.x / LANES; row < RT; row += 128 / LANES) {
-        const int at = r * RT + row, part = threadIdx.x % LANES;
-        if (at >= s.m * a.G) break;
-        float top = -INFINITY;
-        for (int k = ca; k <= cb; ++k) top = fmaxf(top, parts.m[static_cast<size_t>(2 * k + (k == ca)) * RT + row]);
-        float l = 0.0f, v[PART];
-#pragma unroll
-        for (int e = 0; e < PART; ++e) v[e] = 0.0f;
-        for (int k = ca; k <= cb; ++k) {
-            const size_t pr = static_cast<size_t>(2 * k + (k == ca)) * RT + row;
-            const float mk = parts.m[pr], f = (mk == -INFINITY) ? 0.0f : exp2_fast(mk - top);
-            l = fmaf(parts.l[pr], f, l);
-            const float4 x = *reinterpret_cast<const float4 *>(parts.o + pr * DIM + part * PART);
-            const float4 y = *reinterpret_cast<const float4 *>(parts.o + pr * DIM + part * PART + 4);
-            v[0] = fmaf(x.x, f, v[0]); v[1] = fmaf(x.y, f, v[1]); v[2] = fmaf(x.z, f, v[2]); v[3] = fmaf(x.w, f, v[3]);
-            v[4] = fmaf(y.x, f, v[4]); v[5] = fmaf(y.y, f, v[5]); v[6] = fmaf(y.z, f, v[6]); v[7] = fmaf(y.w, f, v[7]);
-        }
-        const float inv = (top == -INFINITY) ? 0.0f : 1.0f / l;
-#pragma unroll
-        for (int e = 0; e < PART; ++e) v[e] *= inv;
-        const long long tq = s.q0 + at / a.G;
-        const int hq = h * a.G + at % a.G;
-        store_row<BF16, PART>(static_cast<__half *>(a.out) + tq * a.o_tok + hq * a.o_head + part * PART, v);
-        if (a.lse && part == 0) a.lse[tq * (c.heads * a.G) + hq] = row_lse(top, l);
-    }
-}
-
-int ctas_of(int sm_count) { return std::min(CTAS_PER_SM * sm_count, MAX_CTAS); }
+int ctas_of(int sm_count) { return std::min(CTAS_PER_SM * sm_count, KV8_MAX_CTAS); }
 
 template <int DIM, int FMT, bool BF16>
 bool launch_rows(const CUtensorMap &km, const CUtensorMap &vm, const Kv8Attend &a, int sm_count, cudaStream_t s) {
@@ -573,12 +425,9 @@ bool launch_rows(const CUtensorMap &km, const CUtensorMap &vm, const Kv8Attend &
 
 }  // namespace
 
-size_t kv8_attend_scratch(int query_rows, int d) {
-    (void)query_rows;
-    return sizeof(float) * 2 * MAX_CTAS * ROWS * (static_cast<size_t>(d) + 2);
-}
+size_t kv8_rows_scratch(int d) { return sizeof(float) * 2 * KV8_MAX_CTAS * ROWS * (static_cast<size_t>(d) + 2); }
 
-int launch_kv8_attend(const Kv8Attend &a, int fmt, int dtype, int sm_count, cudaStream_t s) {
+int launch_kv8_rows(const Kv8Attend &a, int fmt, int dtype, int sm_count, cudaStream_t s) {
     const Kv8 &c = a.c;
     CUtensorMap km, vm;
     const long long rows = (static_cast<long long>(c.num_pages) * c.heads) << c.ps_shift;
@@ -596,18 +445,6 @@ int launch_kv8_attend(const Kv8Attend &a, int fmt, int dtype, int sm_count, cuda
     return ok ? EOSQ_OK : EOSQ_ERR_CUDA;
 }
 
-void launch_kv8_join(const Kv8Attend &a, int dtype, int sm_count, cudaStream_t s) {
-    const int most = (a.max_q * a.G + ROWS - 1) / ROWS;
-    const dim3 grid(static_cast<unsigned>(a.n * most * a.c.heads));
-    const int ctas = ctas_of(sm_count);
-    const bool bf = dtype == EOSQ_BF16;
-    if (a.c.d_shift == 7) {
-        if (bf) launch_dependent(kv8_join_kernel<ROWS, KEYS, 128, true>, grid, 128, 0, s, a, ctas, most);
-        else launch_dependent(kv8_join_kernel<ROWS, KEYS, 128, false>, grid, 128, 0, s, a, ctas, most);
-    } else {
-        if (bf) launch_dependent(kv8_join_kernel<ROWS, KEYS, 64, true>, grid, 128, 0, s, a, ctas, most);
-        else launch_dependent(kv8_join_kernel<ROWS, KEYS, 64, false>, grid, 128, 0, s, a, ctas, most);
-    }
-}
+void launch_kv8_rows_join(const Kv8Attend &a, int dtype, int sm_count, cudaStream_t s) { launch_join<ROWS>(a, dtype, ctas_of(sm_count), s); }
 
 }  // namespace eosq

@@ -273,10 +273,11 @@ def test_queries_of_any_size(ctx):
         out, lse = p.attend(q, [0], [0, rows], scale=1e-3)
         p.attend(q * 1e-30, [0], [0, rows], scale=1e30)
         q[0, 1, 7], q[rows - 1, 2, 3] = float("nan"), float("inf")
-        bad, _ = eosq.eosq_kv8_attend(ctx, p.c, 0, q, _ints([0]), _ints([0, rows]), rows, scale=1e-3, want_lse=True)
+        bad, bad_lse = eosq.eosq_kv8_attend(ctx, p.c, 0, q, _ints([0]), _ints([0, rows]), rows, scale=1e-3, want_lse=True)
         ok = torch.ones((rows, 5), dtype=torch.bool, device="cuda")
         ok[0, 1] = ok[rows - 1, 2] = False
         assert bool(torch.isnan(bad[~ok]).all()) and torch.equal(bad[ok], out[ok])
+        assert bool(torch.isnan(bad_lse[~ok]).all()) and torch.equal(bad_lse[ok], lse[ok])
 
 
 def test_same_bits_every_time_and_on_another_stream(ctx):
