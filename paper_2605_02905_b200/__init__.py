@@ -379,6 +379,9 @@ def eosq_check_status(ctx: Context, cache: Cache, stream=None) -> int:
 
 # ---- 8-bit paged cache ---------------------------------------------------------------------
 
+# These calls are a serving loop's, one per layer and token, so what surrounds the C call is kept short: sizes that follow from the cache are worked
+# out with the handle, tensors are checked by single attributes, and the stream is asked for as a number.
+
 class Kv8Cache:
     """``eosq_kv8_t`` over torch tensors: keys and values of the tokens that no compressed block holds, a byte per number, in
     pages that sequences own through a table in device memory.
@@ -388,7 +391,7 @@ class Kv8Cache:
     once and cannot be replaced.  A new cache is empty: table -1, lengths, refs and flags 0."""
 
     __slots__ = ("k", "v", "k_scale", "v_scale", "table", "lengths", "refs", "flags", "format", "layers", "num_pages", "kv_heads",
-                 "page_size", "d", "max_seqs", "max_pages", "device", "_struct", "_address")
+                 "page_size", "d", "max_seqs", "max_pages", "device", "_struct", "_address", "_index", "_scratch", "_scale")
 
     def __init__(self, *, k, v, k_scale, v_scale, table, lengths, refs, format, flags=None):
         import torch
@@ -413,6 +416,9 @@ class Kv8Cache:
             object.__setattr__(self, name, value)
             setattr(st, name, value)
         object.__setattr__(self, "device", k.device)
+        object.__setattr__(self, "_index", k.get_device())
+        object.__setattr__(self, "_scratch", {})
+        object.__setattr__(self, "_scale", 1.0 / float(np.sqrt(d)))
         object.__setattr__(self, "_struct", st)
         object.__setattr__(self, "_address", ctypes.addressof(st))
 
@@ -432,41 +438,52 @@ class Kv8Cache:
 
 def _kv8_list(cache, t, n, what):
     import torch
-    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.device != cache.device or (n is not None and t.shape[0] != n):
+    if t.dtype is not torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.get_device() != cache._index or (n is not None and t.shape[0] != n):
         raise ValueError(f"{what}: int32 [{n if n is not None else 'n'}] contiguous on {cache.device} is wanted, not {t.dtype} {list(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
 def _kv8_rows(cache, t, heads, what):
     """Data pointer and strides of [total][heads][d], d contiguous."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != cache.d or t.device != cache.device or t.stride(2) != 1:
+    stride = t.stride()
+    if len(stride) != 3 or t.shape[1:] != (heads, cache.d) or t.get_device() != cache._index or stride[2] != 1:
         raise ValueError(f"{what}: [total][{heads}][{cache.d}] with contiguous rows on {cache.device} is wanted, not {list(t.shape)} on {t.device}")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    return t.data_ptr(), stride[0], stride[1]
 
 
 def _any_dtype_code(t):
     import torch
-    if t.dtype == torch.bfloat16:
-        return EOSQ_BF16
-    return _dtype_code(t)
+    return EOSQ_BF16 if t.dtype is torch.bfloat16 else _dtype_code(t)
 
 
-def _empty(shape, dtype, device, stream):
-    """New memory that belongs to the stream it is used on: freed, it goes back to that stream's later work."""
+def _kv8_stream(cache, stream):
+    import torch
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(cache._index)
+
+
+def _new(like, shape, dtype, stream):
+    """Memory on `like`'s device that belongs to the stream it is used on: freed, it goes back to that stream's later work."""
     import torch
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
 
 
 def _kv8_workspace(cache, rows, workspace, stream):
+    """(tensor, address, bytes)"""
     import torch
     if workspace is None:
-        workspace = _empty(max(eosq_kv8_workspace_bytes(cache, rows), 256), torch.uint8, cache.device, stream)
-    elif workspace.device != cache.device or not workspace.is_contiguous():
+        need = cache._scratch.get(rows)
+        if need is None:
+            if len(cache._scratch) > 64:
+                cache._scratch.clear()
+            need = cache._scratch[rows] = max(eosq_kv8_workspace_bytes(cache, rows), 256)
+        workspace = _new(cache.k, need, torch.uint8, stream)
+        return workspace, workspace.data_ptr(), need
+    if workspace.get_device() != cache._index or not workspace.is_contiguous():
         raise ValueError(f"workspace: contiguous memory on {cache.device} is wanted")
-    return workspace
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def eosq_kv8_workspace_bytes(cache: Kv8Cache, query_rows: int = 0) -> int:
@@ -478,9 +495,9 @@ def eosq_kv8_reserve(ctx: Context, cache: Kv8Cache, seqs, add, first=None, strea
     import torch
     n = seqs.shape[0]
     if first is None:
-        first = _empty(n, torch.int32, cache.device, stream)
+        first = _new(seqs, n, torch.int32, stream)
     rc = lib().eosq_kv8_reserve(ctx._h, cache._address, _kv8_list(cache, seqs, None, "seqs"), _kv8_list(cache, add, n, "add"), n,
-                                _kv8_list(cache, first, n, "first"), _stream_ptr(stream))
+                                _kv8_list(cache, first, n, "first"), _kv8_stream(cache, stream))
     _check(rc, "eosq_kv8_reserve", ctx)
     return first
 
@@ -493,7 +510,7 @@ def eosq_kv8_store(ctx: Context, cache: Kv8Cache, layer: int, k, v, seqs, first,
     kp, kt, kh = _kv8_rows(cache, k, cache.kv_heads, "k")
     vp, vt, vh = _kv8_rows(cache, v, cache.kv_heads, "v")
     rc = lib().eosq_kv8_store(ctx._h, cache._address, layer, kp, vp, _any_dtype_code(k), k.shape[0], kt, kh, vt, vh, _kv8_list(cache, seqs, None, "seqs"),
-                              _kv8_list(cache, first, n, "first"), _kv8_list(cache, cu, n + 1, "cu"), n, max_new, _stream_ptr(stream))
+                              _kv8_list(cache, first, n, "first"), _kv8_list(cache, cu, n + 1, "cu"), n, max_new, _kv8_stream(cache, stream))
     _check(rc, "eosq_kv8_store", ctx)
 
 
@@ -507,20 +524,20 @@ def eosq_kv8_attend(ctx: Context, cache: Kv8Cache, layer: int, q, seqs, cu, max_
     G = H // cache.kv_heads
     qp, qt, qh = _kv8_rows(cache, q, H, "q")
     if out is None:
-        out = _empty((total, H, cache.d), q.dtype, q.device, stream)
-    elif out.dtype != q.dtype or out.shape[0] != total:
+        out = _new(q, (total, H, cache.d), q.dtype, stream)
+    elif out.dtype is not q.dtype or out.shape[0] != total:
         raise ValueError(f"out: {q.dtype} [{total}][{H}][{cache.d}] is wanted")
     op, ot, oh = _kv8_rows(cache, out, H, "out")
     if want_lse and lse is None:
-        lse = _empty((total, H), torch.float32, q.device, stream)
+        lse = _new(q, (total, H), torch.float32, stream)
     if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (total, H) or not lse.is_contiguous() or lse.device != cache.device):
         raise ValueError(f"lse: float32 [{total}][{H}] contiguous on {cache.device} is wanted")
-    workspace = _kv8_workspace(cache, max_q * G, workspace, stream)
+    workspace, ws, ws_bytes = _kv8_workspace(cache, min(max_q, total) * G, workspace, stream)
     if scale is None:
-        scale = 1.0 / float(np.sqrt(cache.d))
+        scale = cache._scale
     rc = lib().eosq_kv8_attend(ctx._h, cache._address, layer, qp, _any_dtype_code(q), total, qt, qh, _kv8_list(cache, seqs, None, "seqs"),
                                _kv8_list(cache, cu, n + 1, "cu"), n, max_q, G, scale, int(causal), window, op, ot, oh,
-                               None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+                               None if lse is None else lse.data_ptr(), ws, ws_bytes, _kv8_stream(cache, stream))
     _check(rc, "eosq_kv8_attend", ctx)
     return out if lse is None else (out, lse)
 
@@ -528,14 +545,13 @@ def eosq_kv8_attend(ctx: Context, cache: Kv8Cache, layer: int, q, seqs, cu, max_
 def eosq_kv8_fork(ctx: Context, cache: Kv8Cache, src, dst, workspace=None, stream=None) -> None:
     """Sequence dst[i], empty before, becomes a copy of sequence src[i]; they share whole pages."""
     n = src.shape[0]
-    workspace = _kv8_workspace(cache, 0, workspace, stream)
-    rc = lib().eosq_kv8_fork(ctx._h, cache._address, _kv8_list(cache, src, None, "src"), _kv8_list(cache, dst, n, "dst"), n, workspace.data_ptr(),
-                             workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+    workspace, ws, ws_bytes = _kv8_workspace(cache, 0, workspace, stream)
+    rc = lib().eosq_kv8_fork(ctx._h, cache._address, _kv8_list(cache, src, None, "src"), _kv8_list(cache, dst, n, "dst"), n, ws, ws_bytes, _kv8_stream(cache, stream))
     _check(rc, "eosq_kv8_fork", ctx)
 
 
 def eosq_kv8_free(ctx: Context, cache: Kv8Cache, seqs, stream=None) -> None:
-    rc = lib().eosq_kv8_free(ctx._h, cache._address, _kv8_list(cache, seqs, None, "seqs"), seqs.shape[0], _stream_ptr(stream))
+    rc = lib().eosq_kv8_free(ctx._h, cache._address, _kv8_list(cache, seqs, None, "seqs"), seqs.shape[0], _kv8_stream(cache, stream))
     _check(rc, "eosq_kv8_free", ctx)
 
 
@@ -543,10 +559,9 @@ def eosq_kv8_compact(ctx: Context, cache: Kv8Cache, remap=None, workspace=None, 
     """Moves the used pages to the front of the pool.  Returns where each page went, -1 for one that was free."""
     import torch
     if remap is None:
-        remap = _empty(cache.num_pages, torch.int32, cache.device, stream)
-    workspace = _kv8_workspace(cache, 0, workspace, stream)
-    rc = lib().eosq_kv8_compact(ctx._h, cache._address, _kv8_list(cache, remap, cache.num_pages, "remap"), workspace.data_ptr(),
-                                workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+        remap = _new(cache.refs, cache.num_pages, torch.int32, stream)
+    workspace, ws, ws_bytes = _kv8_workspace(cache, 0, workspace, stream)
+    rc = lib().eosq_kv8_compact(ctx._h, cache._address, _kv8_list(cache, remap, cache.num_pages, "remap"), ws, ws_bytes, _kv8_stream(cache, stream))
     _check(rc, "eosq_kv8_compact", ctx)
     return remap
 
@@ -557,14 +572,14 @@ def eosq_kv8_copy_pages(ctx: Context, from_cache: Kv8Cache, to_cache: Kv8Cache, 
     if from_cache.device != to_cache.device:
         raise ValueError("the caches are on different devices")
     rc = lib().eosq_kv8_copy_pages(ctx._h, from_cache._address, to_cache._address, _kv8_list(from_cache, src_pages, None, "src_pages"),
-                                   _kv8_list(from_cache, dst_pages, n, "dst_pages"), n, _stream_ptr(stream))
+                                   _kv8_list(from_cache, dst_pages, n, "dst_pages"), n, _kv8_stream(from_cache, stream))
     _check(rc, "eosq_kv8_copy_pages", ctx)
 
 
 def eosq_kv8_check(ctx: Context, cache: Kv8Cache, stream=None) -> int:
     """The EOSQ_KV8_* flags that calls on this cache have raised, which are then cleared (synchronises the stream)."""
     flags = ctypes.c_uint32(0)
-    rc = lib().eosq_kv8_check(ctx._h, cache._address, ctypes.byref(flags), _stream_ptr(stream))
+    rc = lib().eosq_kv8_check(ctx._h, cache._address, ctypes.byref(flags), _kv8_stream(cache, stream))
     if rc not in (EOSQ_OK, EOSQ_WARN_BLOCK_STATUS):
         _check(rc, "eosq_kv8_check", ctx)
     return int(flags.value)

@@ -207,18 +207,20 @@ __device__ __forceinline__ int warp_prefix(int *units, int n) {
     return total;
 }
 
+template <bool BF16>
+__device__ __forceinline__ uint32_t pair_bits(float lo, float hi) {
+    if constexpr (BF16) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&b);
+    } else {
+        return half2_bits(lo, hi);
+    }
+}
 template <bool BF16, int N>
 __device__ __forceinline__ void store_row(void *p, const float (&v)[N]) {
     uint32_t w[N / 2];
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i) {
-        if constexpr (BF16) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t *>(&b);
-        } else {
-            w[i] = half2_bits(v[2 * i], v[2 * i + 1]);
-        }
-    }
+    for (int i = 0; i < N / 2; ++i) w[i] = pair_bits<BF16>(v[2 * i], v[2 * i + 1]);
 #pragma unroll
     for (int i = 0; i < N / 8; ++i) reinterpret_cast<uint4 *>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
 }
@@ -294,19 +296,19 @@ __device__ __forceinline__ void kv8_cut(const Kv8Walk<T> &w, int total, int u1, 
     w.a.cuts[blockIdx.x] = cut;
 }
 
-// Row tiles that several CTAs worked on: their partial results under one maximum, in the order of the keys.  A CTA of this kernel per 16 rows and
+// Row tiles that several CTAs worked on: their partial results under one maximum, in the order of the keys.  A CTA of this kernel per 16 rows (or 8) and
 // CTA of the other, which a row tile may begin in and not end.
 template <int RT, int DIM, bool BF16>
 __global__ void __launch_bounds__(128) kv8_join_kernel(const Kv8Attend a, int ctas) {
     pdl_wait();
-    constexpr int PER = RT / 16;
-    const int ca = blockIdx.x / PER, row0 = (blockIdx.x % PER) * 16;
+    constexpr int JOIN = RT < 16 ? RT : 16, PER = RT / JOIN;
+    const int ca = blockIdx.x / PER, row0 = (blockIdx.x % PER) * JOIN;
     const Kv8Cut cut = a.cuts[ca];
     const int rows = cut.m * a.G;
     if (cut.last_cta < 0 || cut.r * RT + row0 >= rows) return;
     const Kv8Parts<RT> parts(a, ctas);
     constexpr int PART = 8, LANES = DIM / PART;   // threads per row
-    for (int row = row0 + threadIdx.x / LANES; row < row0 + 16; row += 128 / LANES) {
+    for (int row = row0 + threadIdx.x / LANES; row < row0 + JOIN; row += 128 / LANES) {
         const int at = cut.r * RT + row, part = threadIdx.x % LANES;
         if (at >= rows) break;
         float top = -INFINITY;
@@ -335,7 +337,7 @@ __global__ void __launch_bounds__(128) kv8_join_kernel(const Kv8Attend a, int ct
 
 template <int RT>
 void launch_join(const Kv8Attend &a, int dtype, int ctas, cudaStream_t s) {
-    const dim3 grid(static_cast<unsigned>(ctas) * (RT / 16));
+    const dim3 grid(static_cast<unsigned>(ctas) * (RT < 16 ? 1 : RT / 16));
     const bool bf = dtype == EOSQ_BF16;
     if (a.c.d_shift == 7) {
         if (bf) launch_dependent(kv8_join_kernel<RT, 128, true>, grid, 128, 0, s, a, ctas);
