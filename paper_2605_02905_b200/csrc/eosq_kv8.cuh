@@ -27,19 +27,15 @@ struct Kv8 {
 constexpr float KV8_SCALE_MIN = 5.421010862427522e-20f;   // 2^-64
 constexpr float KV8_SCALE_MAX = 1.8446744073709552e19f;   // 2^64
 
-// Four codes as fp16, in pairs.  int8: 1024 + 128 + c has c + 128 in its low mantissa bits, so the byte c ^ 0x80 under the
-// exponent byte of 1024 is that number, and one subtraction makes it c, exactly.  e4m3: sign, exponent and mantissa bits
-// moved to fp16's places are 2^-8 of the number (fp16's exponent bias is larger by 8), subnormal numbers included; the
-// factor KV8_UNIT goes with the scale.  (Every byte is then a finite number: what a page holds behind its last token cannot turn a masked weight
-// of 0 into a NaN.)
-template <int FMT> struct Kv8Unit { static constexpr float value = (FMT == EOSQ_KV_E4M3) ? 256.0f : 1.0f; };
+// Four codes as fp16, in pairs, exactly.  int8: 1024 + 128 + c has c + 128 in its low mantissa bits, so the byte c ^ 0x80 under the
+// exponent byte of 1024 is that number, and one subtraction makes it c.  e4m3: an instruction for two (moving sign, exponent and mantissa bits to
+// fp16's places takes eight for four: 231 us for 16 x 32768 tokens, 173 so).  A page behind its last token holds whatever it held: bytes of every
+// kind, among them e4m3's NaNs, whose product with a weight of 0 would be NaN.  Where that can be, no_nan() makes 448 of them.
 __device__ __forceinline__ uint32_t half2_minus(uint32_t a, uint32_t b) {
     uint32_t r;
     asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
-// The two codes in the upper bytes of w's halves (lower bytes 0).
-__device__ __forceinline__ uint32_t e4m3_halves(uint32_t w) { return (w & 0x80008000u) | ((w & 0x7f007f00u) >> 1); }
 template <int FMT>
 __device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t &lo, uint32_t &hi) {
     if constexpr (FMT == EOSQ_KV_INT8) {
@@ -47,9 +43,13 @@ __device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t &lo, uint32_t
         lo = half2_minus(__byte_perm(w, 0x64646464u, 0x4140), 0x64806480u);
         hi = half2_minus(__byte_perm(w, 0x64646464u, 0x4342), 0x64806480u);
     } else {
-        lo = e4m3_halves(__byte_perm(w, 0u, 0x1404));
-        hi = e4m3_halves(__byte_perm(w, 0u, 0x3424));
+        asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
     }
+}
+template <int FMT>
+__device__ __forceinline__ uint32_t no_nan(uint32_t h) {
+    if constexpr (FMT == EOSQ_KV_E4M3) asm("min.f16x2 %0, %1, %2;" : "=r"(h) : "r"(h), "r"(0x5f005f00u));   // (448: of a number and NaN the number)
+    return h;
 }
 
 // ---- a call's sequences -------------------------------------------------------------------------
@@ -98,10 +98,12 @@ struct Kv8Attend {
 };
 
 // The work of one call: every entry's query rows (query t, head g of a KV head: row t * G + g) cut into tiles of RT, the keys that
-// a row tile sees cut into tiles of KT.  A unit is one key tile of one row tile and KV head; units are numbered entry by
-// entry, row tile by row tile, head by head, key tile by key tile.  CTAs take equal runs of them.
-template <int RT, int KT>
+// a row tile sees cut into tiles of KT.  A unit is one key tile of one row tile and KV head, or one of COST that stand for a row tile's beginning and
+// end; units are numbered entry by entry, row tile by row tile, head by head, first those COST, then key tile by key tile.  CTAs take equal runs of
+// them.
+template <int RT, int KT, int COST_>
 struct Kv8Tiles {
+    static constexpr int COST = COST_;
     // Positions [lo, hi) that queries t0 .. t1 of the entry see between them.
     static __device__ __forceinline__ void span(const Kv8Attend &a, const Kv8Seq &s, int t0, int t1, int &lo, int &hi) {
         hi = a.causal ? max(min(s.len, s.len - s.m + t1 + 1), 0) : s.len;
@@ -127,11 +129,13 @@ __device__ __forceinline__ int cta_of(int units, int unit, int ctas) {
 template <typename T>
 struct Kv8Walk {
     const Kv8Attend &a;
-    int i, at, left;                          // entry; units of it that come before; units to go
+    int i, at, left;                                 // entry; units of it that come before; units to go
     Kv8Seq s;
     int row_tiles, r, h, tile0, tiles, from, take;   // now: row tile, head, its key tiles [tile0, tile0 + tiles), of which `take` from `from` on are the run's
+    int reached;                                     // units of the row tile and head up to the run's last
     bool fresh;
-    __device__ __forceinline__ Kv8Walk(const Kv8Attend &a_, int entry, int skip, int units) : a(a_), i(entry), at(skip), left(units), r(0), h(0), tiles(1), fresh(true) {
+    __device__ __forceinline__ Kv8Walk(const Kv8Attend &a_, int entry, int skip, int units)
+        : a(a_), i(entry), at(skip), left(units), s{-1, 0, 0, 0}, r(0), h(0), tile0(0), tiles(1), from(0), take(0), reached(0), fresh(true) {
         if (left > 0) enter();
     }
     __device__ __forceinline__ void enter() {
@@ -140,36 +144,37 @@ struct Kv8Walk {
         r = 0;
     }
     __device__ __forceinline__ bool next() {
-        if (left <= 0) return false;
-        from = 0;
-        if (!fresh && ++h < a.c.heads) {
-            take = min(tiles, left);
-            left -= take;
-            return true;
-        }
-        if (!fresh) ++r;
-        fresh = false;
-        h = 0;
-        while (true) {
-            if (r >= row_tiles) {
-                if (++i >= a.n) {   // (the units say that there is more; unless memory changes under the call)
-                    left = 0;
-                    return false;
+        while (left > 0) {
+            if (fresh || ++h >= a.c.heads) {
+                if (!fresh) ++r;
+                fresh = false;
+                h = 0;
+                while (true) {
+                    if (r >= row_tiles) {
+                        if (++i >= a.n) {   // (the units say that there is more; unless memory changes under the call)
+                            left = take = 0;
+                            return false;
+                        }
+                        enter();
+                        continue;
+                    }
+                    tiles = T::key_tiles(a, s, r, tile0);
+                    const int all = (tiles + T::COST) * a.c.heads;
+                    if (at < all) break;
+                    at -= all;
+                    ++r;
                 }
-                enter();
-                continue;
+                h = at / (tiles + T::COST);
+                at -= h * (tiles + T::COST);
             }
-            tiles = T::key_tiles(a, s, r, tile0);
-            if (at < tiles * a.c.heads) break;
-            at -= tiles * a.c.heads;
-            ++r;
+            reached = at + min(tiles + T::COST - at, left);
+            left -= reached - at;
+            from = max(at - T::COST, 0);
+            take = max(reached - T::COST, 0) - from;
+            at = 0;
+            if (take > 0) return true;
         }
-        h = at / tiles;
-        from = at - h * tiles;
-        at = 0;
-        take = min(tiles - from, left);
-        left -= take;
-        return true;
+        return false;
     }
     // -1: the whole row tile is in the run, else the slot of its partial result: 1 for the run's last, 0 for one that began before.
     __device__ __forceinline__ int slot() const { return (take == tiles) ? -1 : (from == 0 ? 1 : 0); }
@@ -240,7 +245,7 @@ __device__ __forceinline__ Kv8Run kv8_run(const Kv8Attend &a, int *units) {
         if (s.m > 0) {
             const int tiles = T::row_tiles(a, s);
             int first;
-            for (int r = 0; r < tiles; ++r) u += T::key_tiles(a, s, r, first);
+            for (int r = 0; r < tiles; ++r) u += T::key_tiles(a, s, r, first) + T::COST;
         }
         units[i] = u * a.c.heads;
     }
@@ -292,7 +297,7 @@ struct Kv8Parts {
 template <typename T>
 __device__ __forceinline__ void kv8_cut(const Kv8Walk<T> &w, int total, int u1, int ctas) {
     Kv8Cut cut{-1, w.s.q0, w.s.m, w.r, w.h, {0, 0, 0}};
-    if (w.from == 0 && w.take < w.tiles) cut.last_cta = cta_of(total, u1 - w.take + w.tiles - 1, ctas);
+    if (w.from == 0 && w.take > 0 && w.take < w.tiles) cut.last_cta = cta_of(total, u1 - w.reached + T::COST + w.tiles - 1, ctas);
     w.a.cuts[blockIdx.x] = cut;
 }
 

@@ -20,12 +20,12 @@ namespace {
 // 573 instructions for 16 tokens and 286 us for 16 x 32768 tokens.
 constexpr int KEYS = 128, GROUP = 16, GROUPS = KEYS / GROUP;   // tokens of a tile; tokens that are surely in one page
 constexpr int WORKERS = 4, SHARE = KEYS / WORKERS / GROUP, THREADS = 32 * (WORKERS + 1);
-constexpr int CTAS_PER_SM = 2;
+constexpr int CTAS_PER_SM = 2, COST = 2;
 
 struct TileInfo {
-    int first, last;        // of the CTA's run within one row tile
+    int first, last;        // of the CTA's run within one row tile; first = -1: the run has ended, there is no tile
     int tok0;               // the tile's first position
-    int q0, len, m, r, h;   // the entry's queries, its length; row tile, KV head
+    int q0, len, m, h;      // the entry's queries, its length, KV head
     int slot;               // -1: the whole row tile is this CTA's, else the slot of its partial result
     float ks[GROUPS], vlog[GROUPS], vinv[GROUPS];   // per 16 tokens: key scale, log2 of the value scale and its inverse
 };
@@ -77,18 +77,18 @@ __device__ __forceinline__ float query_row(const void *p, uint32_t (&v)[NQ / 2],
     return __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
 }
 
-// NB: query rows in eights (of the 8 NB rows of a row tile).
+// NB: query rows in eights; all rows of an entry and KV head are one row tile.
 template <int DIM, int FMT, bool BF16, int NB>
 __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
                                                                           const Kv8Attend a) {
     constexpr int ROWS = 8 * NB, STAGES = stages_of(DIM, NB);
-    using Tiles = Kv8Tiles<ROWS, KEYS>;
+    using Tiles = Kv8Tiles<ROWS, KEYS, COST>;
     extern __shared__ uint8_t rows_smem[];
-    __shared__ __align__(8) uint64_t full_bar[STAGES], empty_bar[STAGES], join_bar;
+    __shared__ __align__(8) uint64_t full_bar[STAGES], empty_bar[STAGES], put_bar, got_bar;
     __shared__ TileInfo info[STAGES];
     __shared__ volatile int abort_flag;
     __shared__ uint32_t fills[STAGES];
-    __shared__ float top_s[WORKERS][ROWS], sum_s[WORKERS][ROWS];
+    __shared__ float top_s[2][WORKERS][ROWS], sum_s[2][WORKERS][ROWS];
     constexpr int TILE = KEYS * DIM;   // bytes of a tile's keys, or values
     uint8_t *stages = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(rows_smem) + 1023) & ~static_cast<uintptr_t>(1023));
     float4 *sums = reinterpret_cast<float4 *>(stages + STAGES * TILE * 2);
@@ -102,7 +102,8 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
             mbar_init(&empty_bar[s], WORKERS);
             fills[s] = 0;
         }
-        mbar_init(&join_bar, WORKERS);
+        mbar_init(&put_bar, WORKERS);
+        mbar_init(&got_bar, WORKERS);
         abort_flag = 0;
         fence_mbar_init();
     }
@@ -117,7 +118,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
         Kv8Walk<Tiles> w(a, run.entry, run.skip, run.u1 - run.u0);
         int done = 0, at_end = 0;   // tiles of the walk's row tile that are in batches already, and how many it has
         struct Batch {
-            int tiles, tok0, first, last, q0, len, m, r, h, slot;   // uniform; first, last: whether the run's part of a row tile begins, ends here
+            int tiles, tok0, first, last, q0, len, m, h, slot;   // uniform; first, last: whether the run's part of a row tile begins, ends here
             int page;                                               // of this lane's 16 tokens, -1: none
             float ks, vs;
         };
@@ -139,11 +140,10 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
             b.q0 = w.s.q0;
             b.len = w.s.len;
             b.m = w.s.m;
-            b.r = w.r;
             b.h = w.h;
             b.slot = w.slot();
             int lo, hi;
-            Tiles::span(a, w.s, w.r * ROWS / a.G, min(w.s.m - 1, (w.r * ROWS + ROWS - 1) / a.G), lo, hi);
+            Tiles::span(a, w.s, 0, w.s.m - 1, lo, hi);
             const int tok = b.tok0 + lane * GROUP, box0 = tok & ~(box - 1);
             if (lane < b.tiles * GROUPS && box0 < hi && box0 + box > lo) b.page = c.table[static_cast<size_t>(w.s.row) * c.max_pages + (tok >> c.ps_shift)];
             return b;
@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
             if (b.page < 0 || b.page >= c.num_pages) {
                 // -1 stands for "no page is wanted" too: where one is, it is a hole in the table
                 int lo, hi;
-                Tiles::span(a, Kv8Seq{0, b.len, b.m, 0}, b.r * ROWS / a.G, min(b.m - 1, (b.r * ROWS + ROWS - 1) / a.G), lo, hi);
+                Tiles::span(a, Kv8Seq{0, b.len, b.m, 0}, 0, b.m - 1, lo, hi);
                 const int tok = b.tok0 + lane * GROUP, box0 = tok & ~(box - 1);
                 if (lane < b.tiles * GROUPS && box0 < hi && box0 + box > lo) raise(c, EOSQ_KV8_BAD_PAGE);
                 b.page = -1;
@@ -172,8 +172,8 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
         while (ok && now.tiles) {
             if (next.tiles) ask_scales(next);
             const Batch after = next.tiles ? next_batch() : next;
-            const float ks = now.ks * (Kv8Unit<FMT>::value * a.scale_log2);
-            const float vs = fminf(fmaxf(now.vs, KV8_SCALE_MIN), KV8_SCALE_MAX) * Kv8Unit<FMT>::value;
+            const float ks = now.ks * a.scale_log2;
+            const float vs = fminf(fmaxf(now.vs, KV8_SCALE_MIN), KV8_SCALE_MAX);
             const float vlog = now.page >= 0 ? log2f(vs) : -INFINITY, vinv = 1.0f / vs;
             const int tok = now.tok0 + lane * GROUP;
             const bool leader = now.page >= 0 && (tok & (box - 1)) == 0;
@@ -196,7 +196,6 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
                     info[st].q0 = now.q0;
                     info[st].len = now.len;
                     info[st].m = now.m;
-                    info[st].r = now.r;
                     info[st].h = now.h;
                     info[st].slot = now.slot;
                 }
@@ -216,6 +215,15 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
             now = next;
             next = after;
         }
+        if (ok) {
+            const int st = it % STAGES;
+            ok = mbar_wait_warp(&empty_bar[st], ((it / STAGES) & 1u) ^ 1u, &abort_flag);
+            if (ok && lane == 0) {
+                info[st].first = -1;
+                mbar_arrive(&full_bar[st]);
+                fills[st] += 1;
+            }
+        }
         if (lane == 0 && run.u0 < run.u1) kv8_cut(w, run.total, run.u1, run.ctas);
     } else {
         constexpr int STEPS = DIM / 16, WORDS = DIM / 32, OWN = DIM / 4;   // MMA steps over d; words of a token's values per lane; a lane's share of a row
@@ -223,32 +231,36 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
         uint32_t qb[NB][STEPS][2];
         float o[NB][2 * WORDS][4], m[NB][2], l[NB][2], f[NB][2];            // o: channels (8 by 8, two of a word each) x rows 2 q, 2 q + 1
         int lo[NB][2], hi[NB][2], lo_all = 0, hi_all = 0, lo_max = 0, hi_min = 0;
-        uint32_t joins = 0;
+        // Rows are query t of head row - t * G: the same in every row tile.
+        int t_load[NB], h_load[NB], t_row[NB][2], h_row[NB][2];
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            t_load[n] = (8 * n + g) / a.G;
+            h_load[n] = 8 * n + g - t_load[n] * a.G;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                t_row[n][e] = (8 * n + 2 * q + e) / a.G;
+                h_row[n][e] = 8 * n + 2 * q + e - t_row[n][e] * a.G;
+            }
+        }
+        uint32_t items = 0;
         bool ok = true;
-        for (uint32_t it = 0; it < static_cast<uint32_t>(run.u1 - run.u0); ++it) {
+        for (uint32_t it = 0;; ++it) {
             const int st = it % STAGES;
             ok = mbar_wait_warp(&full_bar[st], (it / STAGES) & 1u, &abort_flag);
             if (!ok) break;
             const TileInfo &ti = info[st];
-            const int mq = ti.m, r = ti.r, h = ti.h, rows = mq * a.G, slot = ti.slot, q0 = ti.q0;
+            if (ti.first < 0) break;
+            const int mq = ti.m, h = ti.h, slot = ti.slot, q0 = ti.q0;
             const bool last = ti.last != 0;
             if (ti.first) {
                 const Kv8Seq sq{0, ti.len, mq, 0};
-                auto row_span = [&](int row, int &from, int &to) {
-                    from = to = 0;
-                    if (row < rows) Tiles::span(a, sq, row / a.G, row / a.G, from, to);
-                };
-                const int end = min(rows, r * ROWS + ROWS) - 1;
-                Tiles::span(a, sq, r * ROWS / a.G, end / a.G, lo_all, hi_all);
-                int unused;
-                row_span(r * ROWS, unused, hi_min);
-                row_span(end, lo_max, unused);
 #pragma unroll
                 for (int n = 0; n < NB; ++n) {
-                    const int row = r * ROWS + 8 * n + g;
                     const __half *base = static_cast<const __half *>(a.q);   // (or bf16: two bytes each)
                     uint32_t v[OWN / 2];
-                    const float mine = query_row<BF16, OWN>(base + (q0 + static_cast<long long>(row / a.G)) * a.q_tok + (h * a.G + row % a.G) * a.q_head + q * OWN, v, row < rows);
+                    const float mine =
+                        query_row<BF16, OWN>(base + (q0 + static_cast<long long>(t_load[n])) * a.q_tok + (h * a.G + h_load[n]) * a.q_head + q * OWN, v, t_load[n] < mq);
 #pragma unroll
                     for (int s = 0; s < STEPS; ++s) {
                         qb[n][s][0] = v[2 * s];
@@ -256,14 +268,19 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
                     }
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        f[n][e] = __shfl_sync(0xffffffffu, mine, (2 * q + e) * 4);
-                        row_span(r * ROWS + 8 * n + 2 * q + e, lo[n][e], hi[n][e]);
+                        f[n][e] = BF16 ? __shfl_sync(0xffffffffu, mine, (2 * q + e) * 4) : 1.0f;
+                        lo[n][e] = hi[n][e] = 0;
+                        if (t_row[n][e] < mq) Tiles::span(a, sq, t_row[n][e], t_row[n][e], lo[n][e], hi[n][e]);
                         m[n][e] = -INFINITY;
                         l[n][e] = 0.0f;
                     }
 #pragma unroll
                     for (int b = 0; b < 2 * WORDS; ++b) o[n][b][0] = o[n][b][1] = o[n][b][2] = o[n][b][3] = 0.0f;
                 }
+                Tiles::span(a, sq, 0, mq - 1, lo_all, hi_all);
+                int unused;
+                Tiles::span(a, sq, 0, 0, unused, hi_min);
+                Tiles::span(a, sq, mq - 1, mq - 1, lo_max, unused);
             }
             const int tok = ti.tok0 + warp * SHARE * GROUP;
             if (tok < hi_all && tok + SHARE * GROUP > lo_all) {
@@ -299,7 +316,9 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
                 }
                 // Base-2 logarithms of the weights, value scale included; a row's largest.
                 float top[NB][2];
-                const bool edge = tok < lo_max || tok + SHARE * GROUP > hi_min;
+                bool edge = tok < lo_max || tok + SHARE * GROUP > hi_min;   // some token may be hidden from some row, or not there
+#pragma unroll
+                for (int p = 0; p < SHARE; ++p) edge |= ti.vlog[warp * SHARE + p] == -INFINITY;
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -313,7 +332,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
                                 float x = fmaf(sc[p][n][2 * b + e], k, v);
                                 if (edge) {
                                     const int t = tok + 16 * p + 8 * b + g;
-                                    if (t < lo[n][e] || t >= hi[n][e]) x = -INFINITY;
+                                    if (t < lo[n][e] || t >= hi[n][e] || v == -INFINITY) x = -INFINITY;
                                 }
                                 sc[p][n][2 * b + e] = x;
                                 top[n][e] = fmaxf(top[n][e], x);
@@ -382,6 +401,13 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
                         codes_to_half<FMT>(__byte_perm(w[2][j], w[3][j], 0x5140), va[0][2], va[0][3]);
                         codes_to_half<FMT>(__byte_perm(w[0][j], w[1][j], 0x7362), va[1][0], va[1][1]);
                         codes_to_half<FMT>(__byte_perm(w[2][j], w[3][j], 0x7362), va[1][2], va[1][3]);
+                        if (edge) {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                va[0][k] = no_nan<FMT>(va[0][k]);
+                                va[1][k] = no_nan<FMT>(va[1][k]);
+                            }
+                        }
 #pragma unroll
                         for (int n = 0; n < NB; ++n) {
                             mma_16816(o[n][2 * j], va[0], pb[p][n][0], pb[p][n][1]);
@@ -395,14 +421,8 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
             if (!last) continue;
 
             // The row tile's end: the workers' sums, under one maximum, are added up, a quarter of the channels by each worker (of every lane's: word
-            // by word; at d = 64, half a word).
-            auto together = [&]() {
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&join_bar);
-                ok = mbar_wait_warp(&join_bar, joins & 1u, &abort_flag);
-                joins += 1;
-                return ok;
-            };
+            // by word; at d = 64, half a word).  They are put down once all have read those of the row tile before, and read once all have been put down.
+            const int set = items & 1;
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -411,41 +431,20 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
                     l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], 8);
                     l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], 16);
                     if (g == 0) {
-                        top_s[warp][8 * n + 2 * q + e] = m[n][e];
-                        sum_s[warp][8 * n + 2 * q + e] = l[n][e];
+                        top_s[set][warp][8 * n + 2 * q + e] = m[n][e];
+                        sum_s[set][warp][8 * n + 2 * q + e] = l[n][e];
                     }
                 }
-            if (!together()) break;
             constexpr int QUARTER = 2 * WORDS / 4;   // MMA tiles of 16 channels that a worker adds up
-            float total[NB][2], top[NB][2];
-#pragma unroll
-            for (int n = 0; n < NB; ++n)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int row = 8 * n + 2 * q + e;
-                    float t = top_s[0][row];
-#pragma unroll
-                    for (int w = 1; w < WORKERS; ++w) t = fmaxf(t, top_s[w][row]);
-                    float sum = 0.0f;
-#pragma unroll
-                    for (int w = 0; w < WORKERS; ++w) {
-                        const float mw = top_s[w][row];
-                        sum = fmaf(sum_s[w][row], (mw == -INFINITY) ? 0.0f : exp2_fast(mw - t), sum);
-                    }
-                    top[n][e] = t;
-                    total[n][e] = sum;
-                    const float by = (m[n][e] == -INFINITY) ? 0.0f : exp2_fast(m[n][e] - t);
-#pragma unroll
-                    for (int b = 0; b < 2 * WORDS; ++b) {
-                        o[n][b][e] *= by;
-                        o[n][b][2 + e] *= by;
-                    }
-                }
             // [reader][writer, the reader left out][row eight][tile][lane]
             auto place = [&](int reader, int writer, int n, int b) {
                 return sums + (((reader * (WORKERS - 1) + (writer - (writer > reader ? 1 : 0))) * NB + n) * QUARTER + b) * 32 + lane;
             };
             static_assert(sums_bytes(DIM, NB) == sizeof(float4) * WORKERS * (WORKERS - 1) * NB * QUARTER * 32, "the place of the sums");
+            if (items > 0) {
+                ok = mbar_wait_warp(&got_bar, (items - 1) & 1u, &abort_flag);
+                if (!ok) break;
+            }
 #pragma unroll
             for (int reader = 0; reader < WORKERS; ++reader)
                 if (reader != warp) {
@@ -457,45 +456,65 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
                             *place(reader, warp, n, b) = make_float4(x[0], x[1], x[2], x[3]);
                         }
                 }
-            if (!together()) break;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&put_bar);
+            ok = mbar_wait_warp(&put_bar, items & 1u, &abort_flag);
+            if (!ok) break;
+            float total[NB][2], top[NB][2];
+            float x[NB][QUARTER][4];
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
-                float x[QUARTER][4];
+                float by[WORKERS][2];
 #pragma unroll
-                for (int b = 0; b < QUARTER; ++b)
+                for (int e = 0; e < 2; ++e) {
+                    const int row = 8 * n + 2 * q + e;
+                    float t = top_s[set][0][row];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        x[b][k] = 0.0f;
+                    for (int w = 1; w < WORKERS; ++w) t = fmaxf(t, top_s[set][w][row]);
+                    float sum = 0.0f;
 #pragma unroll
-                        for (int w = 0; w < WORKERS; ++w)
-                            if (w == warp) x[b][k] = o[n][w * QUARTER + b][k];
+                    for (int w = 0; w < WORKERS; ++w) {
+                        const float mw = top_s[set][w][row];
+                        by[w][e] = (mw == -INFINITY) ? 0.0f : exp2_fast(mw - t);
+                        sum = fmaf(sum_s[set][w][row], by[w][e], sum);
                     }
+                    top[n][e] = t;
+                    total[n][e] = sum;
+                }
 #pragma unroll
-                for (int w = 0; w < WORKERS; ++w)
-                    if (w != warp) {
+                for (int b = 0; b < QUARTER; ++b) {
 #pragma unroll
-                        for (int b = 0; b < QUARTER; ++b) {
-                            const float4 y = *place(warp, w, n, b);
-                            x[b][0] += y.x;
-                            x[b][1] += y.y;
-                            x[b][2] += y.z;
-                            x[b][3] += y.w;
-                        }
+                    for (int k = 0; k < 4; ++k) x[n][b][k] = 0.0f;
+#pragma unroll
+                    for (int w = 0; w < WORKERS; ++w) {
+                        float4 y = make_float4(o[n][w * QUARTER + b][0], o[n][w * QUARTER + b][1], o[n][w * QUARTER + b][2], o[n][w * QUARTER + b][3]);
+                        if (w != warp) y = *place(warp, w, n, b);
+                        x[n][b][0] = fmaf(y.x, by[w][0], x[n][b][0]);
+                        x[n][b][1] = fmaf(y.y, by[w][1], x[n][b][1]);
+                        x[n][b][2] = fmaf(y.z, by[w][0], x[n][b][2]);
+                        x[n][b][3] = fmaf(y.w, by[w][1], x[n][b][3]);
                     }
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&got_bar);
+            items += 1;
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
                 // tile b of worker w: channels g * (DIM / 8) + 2 (w QUARTER + b), + 1
                 const int ch = g * (DIM / 8) + 2 * QUARTER * warp;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int row = 8 * n + 2 * q + e, at = r * ROWS + row;
-                    if (at >= rows) continue;
+                    const int row = 8 * n + 2 * q + e;
+                    if (t_row[n][e] >= mq) continue;
                     if (slot < 0) {
                         const float inv = (top[n][e] == -INFINITY) ? 0.0f : 1.0f / total[n][e];
-                        const long long tq = q0 + at / a.G;
-                        const int hq = h * a.G + at % a.G;
+                        const long long tq = q0 + t_row[n][e];
+                        const int hq = h * a.G + h_row[n][e];
                         uint32_t *dst = reinterpret_cast<uint32_t *>(static_cast<__half *>(a.out) + tq * a.o_tok + hq * a.o_head + ch);
                         uint32_t y[QUARTER];
 #pragma unroll
-                        for (int b = 0; b < QUARTER; ++b) y[b] = pair_bits<BF16>(x[b][e] * inv, x[b][2 + e] * inv);
+                        for (int b = 0; b < QUARTER; ++b) y[b] = pair_bits<BF16>(x[n][b][e] * inv, x[n][b][2 + e] * inv);
                         if constexpr (QUARTER == 2) *reinterpret_cast<uint2 *>(dst) = make_uint2(y[0], y[1]);
                         else dst[0] = y[0];
                         if (a.lse && warp == 0 && g == 0) a.lse[tq * (c.heads * a.G) + hq] = row_lse(top[n][e], total[n][e]);
@@ -503,7 +522,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
                         const Kv8Parts<ROWS> parts(a, gridDim.x);
                         const size_t pr = static_cast<size_t>(2 * blockIdx.x + slot) * ROWS + row;
 #pragma unroll
-                        for (int b = 0; b < QUARTER; ++b) *reinterpret_cast<float2 *>(parts.o + pr * DIM + ch + 2 * b) = make_float2(x[b][e], x[b][2 + e]);
+                        for (int b = 0; b < QUARTER; ++b) *reinterpret_cast<float2 *>(parts.o + pr * DIM + ch + 2 * b) = make_float2(x[n][b][e], x[n][b][2 + e]);
                         if (warp == 0 && g == 0) {
                             parts.m[pr] = top[n][e];
                             parts.l[pr] = total[n][e];
@@ -511,7 +530,6 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
                     }
                 }
             }
-            if (!together()) break;
         }
     }
     __syncthreads();

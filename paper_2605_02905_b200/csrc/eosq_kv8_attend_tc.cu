@@ -22,7 +22,8 @@ constexpr int THREADS = 512, LOADER = 8, ISSUER = 12, STAGES = 2, INFOS = 4;
 // Registers a thread after the warps have parted: 256 * 184 + 128 * 104 + 128 * 40 = 512 * 128, what the CTA was launched with.
 constexpr int REGS_ROWS = 184, REGS_LOADER = 104, REGS_ISSUER = 40;
 static_assert(256 * REGS_ROWS + 128 * REGS_LOADER + 128 * REGS_ISSUER <= 512 * 128, "registers of the launch");
-using Tiles = Kv8Tiles<ROWS, KEYS>;
+constexpr int COST = 2;
+using Tiles = Kv8Tiles<ROWS, KEYS, COST>;
 
 struct TileInfo {
     float ks[GROUPS], vlog[GROUPS], vinv[GROUPS];   // per 16 tokens: key scale, log2 of the value scale (-infinity: not there) and its inverse
@@ -146,7 +147,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const Kv8Attend a
                 if (live) Tiles::span(a, w.s, t_of, t_of, lo, hi);
             }
             float m = -INFINITY, l = 0.0f;
-            const float kscale = scale * f * Kv8Unit<FMT>::value;
+            const float kscale = scale * f;
             for (int t = 0; t < w.take; ++t, ++it) {
                 const int slot = it % INFOS;
                 ok = mbar_wait_warp(&info_full[slot], (it / INFOS) & 1u, &abort_flag);
@@ -289,9 +290,11 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const Kv8Attend a
         // The tile whose codes are being asked for: its place in the walk, its pages (lane g of every warp: that of 16 tokens).
         int left_in = 0, tok0 = 0, lo = 0, hi = 0;
         const int32_t *pages = nullptr;
-        auto next_pages = [&]() {   // moves on to the next tile; the page of this lane's 16 tokens, -1 if there is none
+        bool some = true;
+        auto next_pages = [&]() {   // moves on to the next tile, if there is some; the page of this lane's 16 tokens, -1 if there is none
             if (left_in == 0) {
-                if (!w.next()) return -1;
+                some = w.next();
+                if (!some) return -1;
                 left_in = w.take;
                 tok0 = (w.tile0 + w.from) * KEYS;
                 pages = c.table + static_cast<size_t>(w.s.row) * c.max_pages;
@@ -324,7 +327,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const Kv8Attend a
                 }
             }
         };
-        auto put = [&](int kv, uint8_t *dst) {
+        auto put = [&](int kv, uint8_t *dst, bool end) {   // end: some of the tokens may be behind the sequence's last
 #pragma unroll
             for (int k = 0; k < LOADS; ++k) {
                 const int row = k * TOKS + tok_in;
@@ -332,6 +335,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const Kv8Attend a
                 uint32_t z[8];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) codes_to_half<FMT>(y[e], z[2 * e], z[2 * e + 1]);
+                if (end) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] = no_nan<FMT>(z[e]);
+                }
                 uint8_t *line = dst + (part >> 2) * PANEL + row * 128;
                 const int c0 = (part & 3) * 2;
                 const uint4 u = make_uint4(z[0], z[1], z[2], z[3]), v = make_uint4(z[4], z[5], z[6], z[7]);
@@ -341,21 +348,21 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const Kv8Attend a
             fence_proxy_async_smem();
             __syncwarp();
         };
-        const uint32_t units = static_cast<uint32_t>(run.u1 - run.u0);
         bool ok = true;
-        int page = (units > 0) ? next_pages() : -1, head = w.h, at = tok0;
-        if (units > 0) {
+        int page = next_pages(), head = w.h, at = tok0;
+        if (some) {
             ask(0, page, head, at);
             ask(1, page, head, at);
         }
-        for (uint32_t it = 0; it < units && ok; ++it) {
+        for (uint32_t it = 0; some && ok; ++it) {
             const int st = it % STAGES, slot = it % INFOS;
             const uint32_t free_parity = ((it / STAGES) & 1u) ^ 1u;
+            const bool end = at + KEYS > hi;
             float ks = 0.0f, vs = 1.0f, vlog = -INFINITY;
             if (warp == LOADER && lane < GROUPS && page >= 0) {
                 const size_t sc = static_cast<size_t>(page) * c.heads + head;
                 ks = c.scale[0][sc];
-                vs = fminf(fmaxf(c.scale[1][sc], KV8_SCALE_MIN), KV8_SCALE_MAX) * Kv8Unit<FMT>::value;
+                vs = fminf(fmaxf(c.scale[1][sc], KV8_SCALE_MIN), KV8_SCALE_MAX);
                 vlog = log2f(vs);
             }
             page = next_pages();
@@ -374,14 +381,14 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const Kv8Attend a
             }
             ok = mbar_wait_warp(&k_free[st], free_parity, &abort_flag);
             if (!ok) break;
-            put(0, k_smem + st * OPERAND);
+            put(0, k_smem + st * OPERAND, end);
             if (lane == 0) mbar_arrive(&k_full[st]);
-            if (it + 1 < units) ask(0, page, head, at);
+            if (some) ask(0, page, head, at);
             ok = mbar_wait_warp(&v_free[st], free_parity, &abort_flag);
             if (!ok) break;
-            put(1, v_smem + st * OPERAND);
+            put(1, v_smem + st * OPERAND, end);
             if (lane == 0) mbar_arrive(&v_full[st]);
-            if (it + 1 < units) ask(1, page, head, at);
+            if (some) ask(1, page, head, at);
         }
     } else {
         // ---- products -----------------------------------------------------------------------
