@@ -179,6 +179,78 @@ struct Kv8Walk {
     // -1: the whole row tile is in the run, else the slot of its partial result: 1 for the run's last, 0 for one that began before.
     __device__ __forceinline__ int slot() const { return (take == tiles) ? -1 : (from == 0 ? 1 : 0); }
 };
+// A CTA's run of units: first entry, units of it that come before, [u0, u1) of `total`, the runs that there are.
+struct Kv8Run {
+    int entry, skip, u0, u1, total, ctas;
+};
+
+// What a fetching warp asks for ahead of the copies: up to four tiles of 128 tokens of a row tile at a time, a lane for 16 of their tokens (which are in one
+// page): first the page, with the batch after it the scales.
+constexpr int KV8_KEYS = 128, KV8_GROUP = 16, KV8_GROUPS = KV8_KEYS / KV8_GROUP;   // tokens of a tile; tokens of a lane; lanes of a tile
+struct Kv8Batch {
+    int tiles, tok0, first, last, q0, len, m, h, slot, hi;   // uniform; first, last: whether the run's part of a row tile begins, ends here; hi: end of what is seen
+    int page;                                                // of this lane's 16 tokens, -1: none
+    bool wanted;                                             // whether it should have one
+    float ks, vs;
+};
+template <typename T, int RT>
+struct Kv8Fetch {
+    Kv8Walk<T> w;
+    int done, all;   // tiles of the walk's row tile that are in batches already, and how many it has
+    const int lane, box;
+    __device__ __forceinline__ Kv8Fetch(const Kv8Attend &a, const Kv8Run &run, int lane_)
+        : w(a, run.entry, run.skip, run.u1 - run.u0), done(0), all(0), lane(lane_), box(min(a.c.page_size(), KV8_KEYS)) {}
+    __device__ __forceinline__ Kv8Batch next() {
+        const Kv8 &c = w.a.c;
+        Kv8Batch b;
+        b.tiles = 0;
+        b.page = -1;
+        b.wanted = false;
+        if (done == all) {
+            if (!w.next()) return b;
+            done = 0;
+            all = w.take;
+        }
+        b.tiles = min(all - done, 32 / KV8_GROUPS);
+        b.tok0 = (w.tile0 + w.from + done) * KV8_KEYS;
+        b.first = done == 0;
+        done += b.tiles;
+        b.last = done == all;
+        b.q0 = w.s.q0;
+        b.len = w.s.len;
+        b.m = w.s.m;
+        b.h = w.h;
+        b.slot = w.slot();
+        int lo;
+        T::span(w.a, w.s, w.r * RT / w.a.G, min(w.s.m - 1, (w.r * RT + RT - 1) / w.a.G), lo, b.hi);
+        const int tok = b.tok0 + lane * KV8_GROUP, box0 = tok & ~(box - 1);   // a box: what one page gives to a tile
+        b.wanted = lane < b.tiles * KV8_GROUPS && box0 < b.hi && box0 + box > lo;
+        if (b.wanted) b.page = c.table[static_cast<size_t>(w.s.row) * c.max_pages + (tok >> c.ps_shift)];
+        return b;
+    }
+    __device__ __forceinline__ void scales(Kv8Batch &b) {
+        const Kv8 &c = w.a.c;
+        b.ks = 0.0f;
+        b.vs = 1.0f;
+        if (b.page >= 0 && b.page < c.num_pages) {
+            const size_t slot = static_cast<size_t>(b.page) * c.heads + b.h;
+            b.ks = c.scale[0][slot];
+            b.vs = c.scale[1][slot];
+        } else {
+            if (b.wanted) raise(c, EOSQ_KV8_BAD_PAGE);
+            b.page = -1;
+        }
+    }
+    // Whether this lane's page begins a box, and the row of the codes where it does.
+    __device__ __forceinline__ bool leads(const Kv8Batch &b, int &row) const {
+        const Kv8 &c = w.a.c;
+        const int tok = b.tok0 + lane * KV8_GROUP;
+        const bool yes = b.page >= 0 && (tok & (box - 1)) == 0;
+        row = yes ? ((b.page * c.heads + b.h) << c.ps_shift) + (tok & (c.page_size() - 1)) : 0;
+        return yes;
+    }
+};
+
 // Scores are base-2 logarithms; a weight is 2^(x - m + KV8_SHIFT), m being a running maximum that is only moved when a score passes
 // it by more than KV8_SLACK.  So weights are at most 2^14, inside fp16, and those of fp16's smallest normal numbers are 2^-20 of
 // the largest when m is exact.  x contains log2 of the page's value scale, so that the product with the codes of the values needs no
@@ -230,10 +302,6 @@ __device__ __forceinline__ void store_row(void *p, const float (&v)[N]) {
     for (int i = 0; i < N / 8; ++i) reinterpret_cast<uint4 *>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
 }
 
-// A CTA's run of units: first entry, units of it that come before, [u0, u1) of `total`, the runs that there are.
-struct Kv8Run {
-    int entry, skip, u0, u1, total, ctas;
-};
 // Every thread of the CTA (of THREADS) takes part; `units` is shared memory for every entry's units, which may be used otherwise once this has returned.
 template <typename T, int THREADS>
 __device__ __forceinline__ Kv8Run kv8_run(const Kv8Attend &a, int *units) {

@@ -18,7 +18,7 @@ namespace {
 // Both products have the tokens' side as the MMA's larger one: scores are (16 tokens) x (8 query rows), the sums (16 channels) x (8 rows).
 // A product of queries by keys (16 rows, half of them empty with up to 8 heads to a group) would take twice the MMAs, weights and registers: it was
 // 573 instructions for 16 tokens and 286 us for 16 x 32768 tokens.
-constexpr int KEYS = 128, GROUP = 16, GROUPS = KEYS / GROUP;   // tokens of a tile; tokens that are surely in one page
+constexpr int KEYS = KV8_KEYS, GROUP = KV8_GROUP, GROUPS = KV8_GROUPS;
 constexpr int WORKERS = 4, SHARE = KEYS / WORKERS / GROUP, THREADS = 32 * (WORKERS + 1);
 constexpr int CTAS_PER_SM = 2, COST = 2;
 
@@ -113,72 +113,22 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
     __syncthreads();
 
     if (warp == WORKERS) {
-        // Up to four tiles of a row tile at a time, a lane for 16 of their tokens: the pages of the batch after next and the scales of the next one are on
-        // their way while this one's codes are being fetched.
-        Kv8Walk<Tiles> w(a, run.entry, run.skip, run.u1 - run.u0);
-        int done = 0, at_end = 0;   // tiles of the walk's row tile that are in batches already, and how many it has
-        struct Batch {
-            int tiles, tok0, first, last, q0, len, m, h, slot;   // uniform; first, last: whether the run's part of a row tile begins, ends here
-            int page;                                               // of this lane's 16 tokens, -1: none
-            float ks, vs;
-        };
-        const int box = min(c.page_size(), KEYS);   // what one page gives to a tile
-        auto next_batch = [&]() {
-            Batch b;
-            b.tiles = 0;
-            b.page = -1;
-            if (done == at_end) {
-                if (!w.next()) return b;
-                done = 0;
-                at_end = w.take;
-            }
-            b.tiles = min(at_end - done, 32 / GROUPS);
-            b.tok0 = (w.tile0 + w.from + done) * KEYS;
-            b.first = done == 0;
-            done += b.tiles;
-            b.last = done == at_end;
-            b.q0 = w.s.q0;
-            b.len = w.s.len;
-            b.m = w.s.m;
-            b.h = w.h;
-            b.slot = w.slot();
-            int lo, hi;
-            Tiles::span(a, w.s, 0, w.s.m - 1, lo, hi);
-            const int tok = b.tok0 + lane * GROUP, box0 = tok & ~(box - 1);
-            if (lane < b.tiles * GROUPS && box0 < hi && box0 + box > lo) b.page = c.table[static_cast<size_t>(w.s.row) * c.max_pages + (tok >> c.ps_shift)];
-            return b;
-        };
-        auto ask_scales = [&](Batch &b) {
-            b.ks = 0.0f;
-            b.vs = 1.0f;
-            if (b.page < 0 || b.page >= c.num_pages) {
-                // -1 stands for "no page is wanted" too: where one is, it is a hole in the table
-                int lo, hi;
-                Tiles::span(a, Kv8Seq{0, b.len, b.m, 0}, 0, b.m - 1, lo, hi);
-                const int tok = b.tok0 + lane * GROUP, box0 = tok & ~(box - 1);
-                if (lane < b.tiles * GROUPS && box0 < hi && box0 + box > lo) raise(c, EOSQ_KV8_BAD_PAGE);
-                b.page = -1;
-            } else {
-                const size_t slot = static_cast<size_t>(b.page) * c.heads + b.h;
-                b.ks = c.scale[0][slot];
-                b.vs = c.scale[1][slot];
-            }
-        };
+        // The pages of the batch after next and the scales of the next one are on their way while this one's codes are being fetched.
+        Kv8Fetch<Tiles, ROWS> fetch(a, run, lane);
         uint32_t it = 0;
         bool ok = true;
-        Batch now = next_batch();
-        if (now.tiles) ask_scales(now);
-        Batch next = next_batch();
+        Kv8Batch now = fetch.next();
+        if (now.tiles) fetch.scales(now);
+        Kv8Batch next = fetch.next();
         while (ok && now.tiles) {
-            if (next.tiles) ask_scales(next);
-            const Batch after = next.tiles ? next_batch() : next;
+            if (next.tiles) fetch.scales(next);
+            const Kv8Batch after = next.tiles ? fetch.next() : next;
             const float ks = now.ks * a.scale_log2;
             const float vs = fminf(fmaxf(now.vs, KV8_SCALE_MIN), KV8_SCALE_MAX);
             const float vlog = now.page >= 0 ? log2f(vs) : -INFINITY, vinv = 1.0f / vs;
-            const int tok = now.tok0 + lane * GROUP;
-            const bool leader = now.page >= 0 && (tok & (box - 1)) == 0;
+            int row;
+            const bool leader = fetch.leads(now, row);
             const unsigned leaders = __ballot_sync(0xffffffffu, leader);
-            const int row = leader ? ((now.page * c.heads + now.h) << c.ps_shift) + (tok & (c.page_size() - 1)) : 0;
             for (int t = 0; t < now.tiles; ++t, ++it) {
                 const int st = it % STAGES;
                 ok = mbar_wait_warp(&empty_bar[st], ((it / STAGES) & 1u) ^ 1u, &abort_flag);
@@ -201,7 +151,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
                 }
                 __syncwarp();
                 if (lane == 0) {
-                    mbar_arrive_expect_tx(&full_bar[st], __popc((leaders >> (t * GROUPS)) & ((1u << GROUPS) - 1u)) * box * DIM * 2);
+                    mbar_arrive_expect_tx(&full_bar[st], __popc((leaders >> (t * GROUPS)) & ((1u << GROUPS) - 1u)) * fetch.box * DIM * 2);
                     fills[st] += 1;
                 }
                 __syncwarp();
@@ -224,7 +174,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
                 fills[st] += 1;
             }
         }
-        if (lane == 0 && run.u0 < run.u1) kv8_cut(w, run.total, run.u1, run.ctas);
+        if (lane == 0 && run.u0 < run.u1) kv8_cut(fetch.w, run.total, run.u1, run.ctas);
     } else {
         constexpr int STEPS = DIM / 16, WORDS = DIM / 32, OWN = DIM / 4;   // MMA steps over d; words of a token's values per lane; a lane's share of a row
         const int g = lane >> 2, q = lane & 3;                              // g: token, channel or, of the queries, row; q: which part, or which two rows
