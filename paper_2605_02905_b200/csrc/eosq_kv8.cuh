@@ -188,7 +188,7 @@ struct Kv8Run {
 // page): first the page, with the batch after it the scales.
 constexpr int KV8_KEYS = 128, KV8_GROUP = 16, KV8_GROUPS = KV8_KEYS / KV8_GROUP;   // tokens of a tile; tokens of a lane; lanes of a tile
 struct Kv8Batch {
-    int tiles, tok0, first, last, q0, len, m, h, slot, hi;   // uniform; first, last: whether the run's part of a row tile begins, ends here; hi: end of what is seen
+    int tiles, tok0, first, last, q0, len, m, r, h, slot, hi;   // uniform; first, last: whether the run's part of a row tile begins, ends here; hi: end of what is seen
     int page;                                                // of this lane's 16 tokens, -1: none
     bool wanted;                                             // whether it should have one
     float ks, vs;
@@ -219,6 +219,7 @@ struct Kv8Fetch {
         b.q0 = w.s.q0;
         b.len = w.s.len;
         b.m = w.s.m;
+        b.r = w.r;
         b.h = w.h;
         b.slot = w.slot();
         int lo;

@@ -13,24 +13,29 @@ namespace {
 
 // A CTA takes a run of units (Kv8Tiles): 256 query rows, in two halves of 128, against tiles of 128 tokens.
 //   warps 0-3, 4-7   the halves' weights, a row per thread: scores out of tensor memory, weights back into it (in the scores' place, as the
-//                    A operand of the second product), maximum and sum in registers; queries in, results out
+//                    A operand of the second product), maximum and sum in registers; results out
 //   warps 8-11       turn codes into fp16 operands
 //   warp 12          issues the products; while one half's weights are made, the other half's products run
-//   warp 13          fetches codes, a tile ahead, and the scales
+//   warp 13          walks through the run, tells the others about each tile, and fetches codes, a tile ahead, and scales
+//   warps 14, 15     bring the next row tile's queries in as soon as this one's last scores have been made
 // The weights are the bottleneck: 2^x of 128 x 256 scores is 2048 cycles of an SM's special function units, as many as the two products take.
 constexpr int ROWS = 256, HALF = 128, KEYS = KV8_KEYS, GROUP = KV8_GROUP, GROUPS = KV8_GROUPS;
-constexpr int LOADER = 8, ISSUER = 12, FETCHER = 13, THREADS = 32 * 14, STAGES = 2, INFOS = 4;
+constexpr int LOADER = 8, ISSUER = 12, FETCHER = 13, THREADS = 32 * 16, STAGES = 2, INFOS = 4;
 constexpr int COST = 2;
 using Tiles = Kv8Tiles<ROWS, KEYS, COST>;
 
 struct TileInfo {
-    int end;   // 1: some of the tokens may be behind the sequence's last; -1: the run has ended, there is no tile
+    int end;                // 1: some of the tokens may be behind the sequence's last; -1: the run has ended, there is no tile
+    int first, last;        // of the CTA's run within one row tile
+    int tok0;               // the tile's first position
+    int q0, len, m, r, h;   // the entry's queries, its length; row tile, KV head
+    int slot;               // -1: the whole row tile is this CTA's, else the slot of its partial result
     float ks[GROUPS], vlog[GROUPS], vinv[GROUPS];   // per 16 tokens: key scale, log2 of the value scale (-infinity: not there) and its inverse
 };
 
 constexpr size_t operand_bytes(int d) { return static_cast<size_t>(HALF) * d * 2; }   // 128 rows of fp16
 constexpr size_t smem_bytes(int d) { return 1024 + (2 + 2 * STAGES) * operand_bytes(d) + 2 * static_cast<size_t>(KEYS) * d; }
-static_assert(smem_bytes(128) + 1400 <= 232448, "shared memory of a CTA, with the barriers and scales");
+static_assert(smem_bytes(128) + 1700 <= 232448, "shared memory of a CTA, with the barriers and scales");
 static_assert(2 * STAGES * operand_bytes(64) >= sizeof(int) * EOSQ_KV8_MAX_SEQS, "units of every entry");
 
 __device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
@@ -50,13 +55,20 @@ __device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
     return r;
 }
 
+__device__ __forceinline__ uint64_t desc_of(uint32_t lo, uint32_t hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+    return r;
+}
+
 template <int DIM, int FMT, bool BF16>
 __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
                                                                   const Kv8Attend a) {
     extern __shared__ uint8_t tiles_smem[];
-    __shared__ __align__(8) uint64_t q_full[2], s_full[2], p_full[2], o_done[2], k_full[STAGES], v_full[STAGES], k_free[STAGES], v_free[STAGES], info_full[INFOS],
+    __shared__ __align__(8) uint64_t q_full[2], q_free[2], s_full[2], p_full[2], o_done[2], k_full[STAGES], v_full[STAGES], k_free[STAGES], v_free[STAGES], info_full[INFOS],
         info_free[INFOS], code_full[2], code_free[2], drain_bar;
     __shared__ TileInfo info[INFOS];
+    __shared__ int8_t q_exp[2][ROWS];   // by row tile in turn: the power of two that its queries were divided by
     __shared__ uint32_t tmem_base_s;
     __shared__ volatile int abort_flag;
     __shared__ uint32_t fills[2];   // of keys, of values
@@ -71,7 +83,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
         for (int i = 0; i < 2; ++i) {
             mbar_init(&code_full[i], 1);
             mbar_init(&code_free[i], 4);
-            mbar_init(&q_full[i], 4);
+            mbar_init(&q_full[i], 2);
+            mbar_init(&q_free[i], 1);
             mbar_init(&s_full[i], 1);
             mbar_init(&p_full[i], 4);
             mbar_init(&o_done[i], 1);
@@ -84,7 +97,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
         }
         for (int i = 0; i < INFOS; ++i) {
             mbar_init(&info_full[i], 1);
-            mbar_init(&info_free[i], 12);
+            mbar_init(&info_free[i], 15);   // all warps but the one that fills them
         }
         mbar_init(&drain_bar, 1);
         abort_flag = 0;
@@ -108,207 +121,180 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
         const int half = warp >> 2, row_in = (warp & 3) * 32 + lane;
         const uint32_t s_at = tmem + half * KEYS + (static_cast<uint32_t>((warp & 3) * 32) << 16), o_at = s_at - half * KEYS + 256 + half * DIM;
         const float scale = fabsf(a.scale_log2);
-        uint8_t *q_mine = q_smem + half * OPERAND + row_in * 128;
-        Kv8Walk<Tiles> w(a, run.entry, run.skip, run.u1 - run.u0);
-        uint32_t it = 0, s_phase = 0, o_phase = 0;
-        bool ok = true;
-        while (ok && w.next()) {
-            const int row = w.r * ROWS + half * HALF + row_in, rows = w.s.m * a.G;
-            const bool active = w.r * ROWS + half * HALF < rows, live = row < rows;   // (active: some row of this half)
-            const int t_of = live ? row / a.G : 0, hq = w.h * a.G + (live ? row % a.G : 0);
-            int lo = 0, hi = 0;
-            float f = 1.0f;
-            if (active) {
-                // The queries: this row's, as fp16; bf16 rows brought to its range (query_row does the same for a quarter of a row).  The scale's sign goes with them.
-                const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __half *>(a.q) + (w.s.q0 + static_cast<long long>(t_of)) * a.q_tok + hq * a.q_head);
-                float g = 1.0f;
-                if constexpr (BF16) {
-                    float top = 0.0f;
-                    if (live) {
-#pragma unroll 4
-                        for (int k = 0; k < DIM / 8; ++k) {
-                            const uint4 v = src[k];
-                            const uint32_t x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(x[e] << 16)), fabsf(__uint_as_float(x[e] & 0xffff0000u))));
-                        }
-                    }
-                    const int e2 = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 14, -100), 100);
-                    g = __uint_as_float(static_cast<uint32_t>(127 - e2) << 23);
-                    f = __uint_as_float(static_cast<uint32_t>(127 + e2) << 23);
-                }
-                const uint32_t flip = (a.scale_log2 < 0.0f) ? 0x80008000u : 0u;
-#pragma unroll 4
-                for (int k = 0; k < DIM / 8; ++k) {
-                    const uint4 v = live ? src[k] : make_uint4(0, 0, 0, 0);
-                    uint32_t x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if constexpr (BF16) x[e] = half2_bits(__uint_as_float(x[e] << 16) * g, __uint_as_float(x[e] & 0xffff0000u) * g);
-                        x[e] ^= flip;
-                    }
-                    *reinterpret_cast<uint4 *>(q_mine + (k >> 3) * PANEL + (((k & 7) ^ (row_in & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
-                }
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&q_full[half]);
-                if (live) Tiles::span(a, w.s, t_of, t_of, lo, hi);
-            }
-            float m = -INFINITY, l = 0.0f;
-            const float kscale = scale * f;
-            for (int t = 0; t < w.take; ++t, ++it) {
-                const int slot = it % INFOS;
-                ok = mbar_wait_warp(&info_full[slot], (it / INFOS) & 1u, &abort_flag);
-                if (!ok) break;
-                if (active) {
-                    const TileInfo &ti = info[slot];
-                    ok = mbar_wait_warp(&s_full[half], s_phase & 1u, &abort_flag);
-                    if (!ok) break;
-                    s_phase += 1;
-                    tc_fence_after_sync();
-                    const int tok0 = (w.tile0 + w.from + t) * KEYS;
-                    const bool edge = __any_sync(0xffffffffu, live && (tok0 < lo || tok0 + KEYS > hi));
-                    // A row's base-2 logarithms are s * ks + vlog, with a key and a value scale for every 16 tokens.  (ks is kept above
-                    // zero, so that masked scores stay -infinity under a scale of zero.)  The scores are read twice, 32 at a time: first the largest, ...
-                    auto masked = [&](uint32_t (&x)[32], int at) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (at + e < lo || at + e >= hi) x[e] = 0xff800000u;   // -infinity
-                    };
-                    auto ks_of = [&](int g) { return fmaxf(ti.ks[g] * kscale, 1e-37f); };
-                    float top = -INFINITY;
-                    auto largest = [&](uint32_t (&x)[32], int k) {
-                        if (edge) masked(x, tok0 + 32 * k);
-#pragma unroll
-                        for (int gg = 0; gg < 2; ++gg) {
-                            float t0 = __uint_as_float(x[16 * gg]), t1 = __uint_as_float(x[16 * gg + 1]);
-#pragma unroll
-                            for (int e = 2; e < GROUP; e += 2) {
-                                t0 = fmaxf(t0, __uint_as_float(x[16 * gg + e]));
-                                t1 = fmaxf(t1, __uint_as_float(x[16 * gg + e + 1]));
-                            }
-                            const int g = 2 * k + gg;
-                            top = fmaxf(top, fmaf(fmaxf(t0, t1), ks_of(g), ti.vlog[g]));
-                        }
-                    };
-                    uint32_t x[32], y[32];
-                    tmem_ld32(s_at, x);
-                    tmem_ld_wait(x);
-#pragma unroll 1
-                    for (int k = 0; k < KEYS / 32; k += 2) {
-                        tmem_ld32(s_at + 32 * (k + 1), y);
-                        largest(x, k);
-                        tmem_ld_wait(y);
-                        tmem_ld32(s_at + 32 * ((k + 2) % (KEYS / 32)), x);   // (at the end the first ones again)
-                        largest(y, k + 1);
-                        tmem_ld_wait(x);
-                    }
-                    if (__any_sync(0xffffffffu, top > m + KV8_SLACK)) {
-                        const float n = fmaxf(m, top), by = (n == -INFINITY) ? 1.0f : exp2_fast(m - n);
-                        m = n;
-                        l *= by;
-                        if (t > 0) {   // the products before have completed: the issuer's scores of this tile came behind them
-#pragma unroll 1
-                            for (int k = 0; k < DIM / 32; ++k) {
-                                uint32_t o[32];
-                                tmem_ld32(o_at + 32 * k, o);
-                                tmem_ld_wait(o);
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
-                                tmem_st32(o_at + 32 * k, o);
-                            }
-                        }
-                    }
-                    const float b = (m == -INFINITY) ? 0.0f : KV8_SHIFT - m;
-                    // Below, s * ks + (vlog - m + shift) is rounded once, m before: of logarithms beyond 2^22 the difference could pass fp16's range.  There
-                    // every logarithm is rounded as m was.
-                    const bool far = __any_sync(0xffffffffu, fabsf(m) > 4194304.0f && m != -INFINITY);
-                    // ... then the weights, 32 of them into the place of 16 scores that have been read.
-                    auto weights = [&](uint32_t (&x)[32], int k) {
-                        if (edge) masked(x, tok0 + 32 * k);
-                        uint32_t p[16];
-#pragma unroll
-                        for (int gg = 0; gg < 2; ++gg) {
-                            const int g = 2 * k + gg;
-                            float kf = ks_of(g), cf = ti.vlog[g] + b;
-                            if (far) {
-#pragma unroll
-                                for (int e = 0; e < GROUP; ++e) x[16 * gg + e] = __float_as_uint(fmaf(__uint_as_float(x[16 * gg + e]), kf, ti.vlog[g]));
-                                kf = 1.0f;
-                                cf = b;
-                            }
-                            const uint64_t k2 = pair_of(kf, kf), c2 = pair_of(cf, cf);
-                            uint64_t sum = 0;
-#pragma unroll
-                            for (int e = 0; e < GROUP; e += 2) {
-                                float y0, y1;
-                                unpair(fma_pair(pair_of(__uint_as_float(x[16 * gg + e]), __uint_as_float(x[16 * gg + e + 1])), k2, c2), y0, y1);
-                                y0 = exp2_fast(y0);
-                                y1 = exp2_fast(y1);
-                                sum = add_pair(sum, pair_of(y0, y1));
-                                p[8 * gg + (e >> 1)] = half2_bits(y0, y1);
-                            }
-                            float s0, s1;
-                            unpair(sum, s0, s1);
-                            l = fmaf(s0 + s1, ti.vinv[g], l);
-                        }
-                        tmem_st16(s_at + 16 * k, p);
-                    };
-#pragma unroll 1
-                    for (int k = 0; k < KEYS / 32; k += 2) {
-                        tmem_ld32(s_at + 32 * (k + 1), y);
-                        weights(x, k);
-                        tmem_ld_wait(y);
-                        if (k + 2 < KEYS / 32) tmem_ld32(s_at + 32 * (k + 2), x);
-                        weights(y, k + 1);
-                        tmem_ld_wait(x);
-                    }
-                    tmem_st_wait();
-                    tc_fence_before_sync();
-                }
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(&info_free[slot]);
-                    if (active) mbar_arrive(&p_full[half]);
-                }
-            }
+        uint32_t tiles_done = 0, items_done = 0, items = 0;   // tiles and row tiles of this half, row tiles in all
+        int lo = 0, hi = 0;
+        bool ok = true, active = false, live = false;   // (active: some row of this half is a query)
+        float m = -INFINITY, l = 0.0f, kscale = scale;
+        for (uint32_t it = 0;; ++it) {
+            const int slot = it % INFOS;
+            ok = mbar_wait_warp(&info_full[slot], (it / INFOS) & 1u, &abort_flag);
             if (!ok) break;
-            if (!active) continue;
-            ok = mbar_wait_warp(&o_done[half], o_phase & 1u, &abort_flag);
-            if (!ok) break;
-            o_phase += 1;
-            tc_fence_after_sync();
-            const int slot = w.slot();
-            const float inv = (slot >= 0) ? 1.0f : (m == -INFINITY ? 0.0f : 1.0f / l);
-            const long long tq = w.s.q0 + static_cast<long long>(t_of);
-            const Kv8Parts<ROWS> parts(a, gridDim.x);
-            const size_t pr = static_cast<size_t>(2 * blockIdx.x + max(slot, 0)) * ROWS + half * HALF + row_in;
-#pragma unroll 1
-            for (int k = 0; k < DIM / 32; ++k) {
-                uint32_t o[32];
-                float v[32];
-                tmem_ld32(o_at + 32 * k, o);
-                tmem_ld_wait(o);
-#pragma unroll
-                for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(o[e]) * inv;
+            const TileInfo &ti = info[slot];
+            if (ti.end < 0) break;
+            const bool first = ti.first != 0, last = ti.last != 0;
+            if (first) {
+                const int row0 = ti.r * ROWS + half * HALF, rows = ti.m * a.G;
+                active = row0 < rows;
+                live = row0 + row_in < rows;
+                lo = hi = 0;
                 if (live) {
-                    if (slot < 0) {
-                        store_row<BF16, 32>(static_cast<__half *>(a.out) + tq * a.o_tok + hq * a.o_head + 32 * k, v);
-                    } else {
+                    const int t = (row0 + row_in) / a.G;
+                    Tiles::span(a, Kv8Seq{0, ti.len, ti.m, 0}, t, t, lo, hi);
+                }
+                m = -INFINITY;
+                l = 0.0f;
+            }
+            if (active) {
+                const int tok0 = ti.tok0;
+                const bool edge = __any_sync(0xffffffffu, live && (tok0 < lo || tok0 + KEYS > hi));
+                ok = mbar_wait_warp(&s_full[half], tiles_done & 1u, &abort_flag);
+                if (!ok) break;
+                tiles_done += 1;
+                tc_fence_after_sync();
+                if (BF16 && first) kscale = scale * __uint_as_float(static_cast<uint32_t>(127 + q_exp[items & 1][half * HALF + row_in]) << 23);
+                // A row's base-2 logarithms are s * ks + vlog, with a key and a value scale for every 16 tokens.  (ks is kept above zero, so that masked scores stay
+                // -infinity under a scale of zero.)  The scores are read twice, 32 at a time: all 128 in registers, in straight code, took longer.  First the largest, ...
+                auto ks_of = [&](int g) { return fmaxf(ti.ks[g] * kscale, 1e-37f); };
+                auto hide = [&](uint32_t (&x)[32], int at) {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4 *>(parts.o + pr * DIM + 32 * k + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                    for (int e = 0; e < 32; ++e)
+                        if (at + e < lo || at + e >= hi) x[e] = 0xff800000u;   // -infinity
+                };
+                float top = -INFINITY;
+                auto largest = [&](uint32_t (&x)[32], int k) {
+                    if (edge) hide(x, tok0 + 32 * k);
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        float t0 = __uint_as_float(x[16 * g]), t1 = __uint_as_float(x[16 * g + 1]);
+#pragma unroll
+                        for (int e = 2; e < GROUP; e += 2) {
+                            t0 = fmaxf(t0, __uint_as_float(x[16 * g + e]));
+                            t1 = fmaxf(t1, __uint_as_float(x[16 * g + e + 1]));
+                        }
+                        top = fmaxf(top, fmaf(fmaxf(t0, t1), ks_of(2 * k + g), ti.vlog[2 * k + g]));
+                    }
+                };
+                uint32_t x[32], y[32];
+                tmem_ld32(s_at, x);
+                tmem_ld_wait(x);
+#pragma unroll 1
+                for (int k = 0; k < KEYS / 32; k += 2) {
+                    tmem_ld32(s_at + 32 * (k + 1), y);
+                    largest(x, k);
+                    tmem_ld_wait(y);
+                    tmem_ld32(s_at + 32 * ((k + 2) % (KEYS / 32)), x);   // (at the end the first ones again)
+                    largest(y, k + 1);
+                    tmem_ld_wait(x);
+                }
+                if (__any_sync(0xffffffffu, top > m + KV8_SLACK)) {
+                    const float n = fmaxf(m, top), by = (n == -INFINITY) ? 1.0f : exp2_fast(m - n);
+                    m = n;
+                    l *= by;
+                    if (!first) {   // the sums so far: the products that made them have ended, the scores came behind them
+#pragma unroll 1
+                        for (int k = 0; k < DIM / 32; ++k) {
+                            uint32_t o[32];
+                            tmem_ld32(o_at + 32 * k, o);
+                            tmem_ld_wait(o);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
+                            tmem_st32(o_at + 32 * k, o);
+                        }
                     }
                 }
-            }
-            if (live) {
-                if (slot >= 0) {
-                    parts.m[pr] = m;
-                    parts.l[pr] = l;
-                } else if (a.lse) {
-                    a.lse[tq * (c.heads * a.G) + hq] = row_lse(m, l);
+                const float b = (m == -INFINITY) ? 0.0f : KV8_SHIFT - m;
+                // Below, s * ks + (vlog - m + shift) is rounded once, m before: of logarithms beyond 2^22 the difference could pass fp16's range.  There
+                // every logarithm is rounded as m was.
+                const bool far = __any_sync(0xffffffffu, fabsf(m) > 4194304.0f && m != -INFINITY);
+                // ... then for the weights, 32 of them into the place of 16 scores that have been read.
+                auto weights = [&](uint32_t (&x)[32], int k) {
+                    if (edge) hide(x, tok0 + 32 * k);
+                    uint32_t p[16];
+#pragma unroll
+                    for (int gg = 0; gg < 2; ++gg) {
+                        const int g = 2 * k + gg;
+                        float kf = ks_of(g), cf = ti.vlog[g] + b;
+                        if (far) {
+#pragma unroll
+                            for (int e = 0; e < GROUP; ++e) x[16 * gg + e] = __float_as_uint(fmaf(__uint_as_float(x[16 * gg + e]), kf, ti.vlog[g]));
+                            kf = 1.0f;
+                            cf = b;
+                        }
+                        const uint64_t k2 = pair_of(kf, kf), c2 = pair_of(cf, cf);
+                        uint64_t sum = 0;
+#pragma unroll
+                        for (int e = 0; e < GROUP; e += 2) {
+                            float y0, y1;
+                            unpair(fma_pair(pair_of(__uint_as_float(x[16 * gg + e]), __uint_as_float(x[16 * gg + e + 1])), k2, c2), y0, y1);
+                            y0 = exp2_fast(y0);
+                            y1 = exp2_fast(y1);
+                            sum = add_pair(sum, pair_of(y0, y1));
+                            p[8 * gg + (e >> 1)] = half2_bits(y0, y1);
+                        }
+                        float s0, s1;
+                        unpair(sum, s0, s1);
+                        l = fmaf(s0 + s1, ti.vinv[g], l);
+                    }
+                    tmem_st16(s_at + 16 * k, p);
+                };
+#pragma unroll 1
+                for (int k = 0; k < KEYS / 32; k += 2) {
+                    tmem_ld32(s_at + 32 * (k + 1), y);
+                    weights(x, k);
+                    tmem_ld_wait(y);
+                    if (k + 2 < KEYS / 32) tmem_ld32(s_at + 32 * (k + 2), x);
+                    weights(y, k + 1);
+                    tmem_ld_wait(x);
                 }
+                tmem_st_wait();
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full[half]);
             }
-            tc_fence_before_sync();
+            if (last) items += 1;
+            if (last && active) {
+                const int row = ti.r * ROWS + half * HALF + row_in, place = ti.slot;
+                const int t_of = row / a.G, hq = ti.h * a.G + row - t_of * a.G;
+                const long long tq = ti.q0 + static_cast<long long>(t_of);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&info_free[slot]);
+                ok = mbar_wait_warp(&o_done[half], items_done & 1u, &abort_flag);
+                items_done += 1;
+                if (!ok) break;
+                tc_fence_after_sync();
+                const float inv = (place >= 0) ? 1.0f : (m == -INFINITY ? 0.0f : 1.0f / l);
+                const Kv8Parts<ROWS> parts(a, gridDim.x);
+                const size_t pr = static_cast<size_t>(2 * blockIdx.x + max(place, 0)) * ROWS + half * HALF + row_in;
+#pragma unroll 1
+                for (int k = 0; k < DIM / 32; ++k) {
+                    uint32_t o[32];
+                    float v[32];
+                    tmem_ld32(o_at + 32 * k, o);
+                    tmem_ld_wait(o);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(o[e]) * inv;
+                    if (live) {
+                        if (place < 0) {
+                            store_row<BF16, 32>(static_cast<__half *>(a.out) + tq * a.o_tok + hq * a.o_head + 32 * k, v);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4 *>(parts.o + pr * DIM + 32 * k + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                        }
+                    }
+                }
+                if (live) {
+                    if (place >= 0) {
+                        parts.m[pr] = m;
+                        parts.l[pr] = l;
+                    } else if (a.lse) {
+                        a.lse[tq * (c.heads * a.G) + hq] = row_lse(m, l);
+                    }
+                }
+                tc_fence_before_sync();
+            } else {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&info_free[slot]);
+            }
         }
     } else if (warp < ISSUER) {
         // ---- keys and values ----------------------------------------------------------------
@@ -365,74 +351,180 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
         }
     } else if (warp == ISSUER) {
         // ---- products -----------------------------------------------------------------------
-        {
-            constexpr uint32_t idesc_s = umma_idesc_f16(HALF, KEYS, false, false), idesc_o = umma_idesc_f16(HALF, DIM, false, true);
-            const bool issuer = elect_one();
-            Kv8Walk<Tiles> w(a, run.entry, run.skip, run.u1 - run.u0);
-            uint32_t it = 0, q_phase = 0, p_phase[2] = {0, 0};
-            uint32_t q_phases[2] = {0, 0};
-            bool ok = true;
-            (void)q_phase;
-            const uint32_t q_addr = smem_u32(q_smem), k_addr = smem_u32(k_smem), v_addr = smem_u32(v_smem);
-            // Scores of one half against the keys of stage st.
-            auto scores = [&](int half, int st) {
-                if (issuer) {
+        constexpr uint32_t idesc_s = umma_idesc_f16(HALF, KEYS, false, false), idesc_o = umma_idesc_f16(HALF, DIM, false, true);
+        const bool issuer = elect_one();
+        uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0};   // row tiles, tiles of each half
+        bool ok = true;
+        // An operand's descriptor: its lower word counts addresses in 16 bytes, so that a step along the operand is an addition there; the upper one is the same for all.
+        const uint64_t any_desc = umma_desc_sw128(0, 0, 1024);
+        const uint32_t hi_desc = static_cast<uint32_t>(any_desc >> 32);
+        const uint32_t q_desc = smem_u32(q_smem) >> 4, k_desc = smem_u32(k_smem) >> 4, v_desc = (smem_u32(v_smem) >> 4) | ((PANEL >> 4) << 16);
+        auto scores = [&](int half, int st) {
+            const uint32_t q = q_desc + half * (OPERAND >> 4), kd = k_desc + st * (OPERAND >> 4), to = tmem + half * KEYS;
+            if (issuer) {
 #pragma unroll
-                    for (int k = 0; k < DIM / 16; ++k) {
-                        const uint32_t off = (k >> 2) * PANEL + (k & 3) * 32;
-                        umma_f16(tmem + half * KEYS, umma_desc_sw128(q_addr + half * OPERAND + off, 16, 1024), umma_desc_sw128(k_addr + st * OPERAND + off, 16, 1024), idesc_s,
-                                 k ? 1u : 0u);
-                    }
-                    umma_commit(&s_full[half]);
+                for (int k = 0; k < DIM / 16; ++k) {
+                    constexpr uint32_t panel = PANEL >> 4;
+                    umma_f16(to, desc_of(q + (k >> 2) * panel + (k & 3) * 2, hi_desc), desc_of(kd + (k >> 2) * panel + (k & 3) * 2, hi_desc), idesc_s, k ? 1u : 0u);
                 }
-                __syncwarp();
-            };
-            auto values = [&](int half, int st, bool first) {
-                if (issuer) {
-#pragma unroll
-                    for (int k = 0; k < KEYS / 16; ++k)
-                        umma_f16_ts(tmem + 256 + half * DIM, tmem + half * KEYS + 8 * k, umma_desc_sw128(v_addr + st * OPERAND + k * 2048, PANEL, 1024), idesc_o,
-                                    (first && k == 0) ? 0u : 1u);
-                }
-                __syncwarp();
-            };
-            auto commit = [&](uint64_t *bar) {
-                if (issuer) umma_commit(bar);
-                __syncwarp();
-            };
-            while (ok && w.next()) {
-                const bool two = w.r * ROWS + HALF < w.s.m * a.G;
-                const int halves = two ? 2 : 1;
-                for (int t = -1; t < w.take && ok; ++t) {
-                    // the values of tile t, then the scores of tile t + 1, one half after the other
-                    const bool more = t + 1 < w.take;
-                    const uint32_t kt = it + t + 1, vt = it + t;
-                    if (more) ok = mbar_wait_warp(&k_full[kt % STAGES], (kt / STAGES) & 1u, &abort_flag);
-                    if (ok && t >= 0) ok = mbar_wait_warp(&v_full[vt % STAGES], (vt / STAGES) & 1u, &abort_flag);
-                    for (int half = 0; half < halves && ok; ++half) {
-                        if (t < 0) {
-                            ok = mbar_wait_warp(&q_full[half], q_phases[half] & 1u, &abort_flag);
-                            q_phases[half] += 1;
-                        } else {
-                            ok = mbar_wait_warp(&p_full[half], p_phase[half] & 1u, &abort_flag);
-                            p_phase[half] += 1;
-                        }
-                        if (!ok) break;
-                        tc_fence_after_sync();
-                        if (t >= 0) values(half, vt % STAGES, t == 0);
-                        if (t >= 0 && half == halves - 1) commit(&v_free[vt % STAGES]);
-                        if (more) {
-                            scores(half, kt % STAGES);
-                            if (half == halves - 1) commit(&k_free[kt % STAGES]);
-                        } else {
-                            commit(&o_done[half]);
-                        }
-                    }
-                }
-                it += w.take;
+                umma_commit(&s_full[half]);
             }
+            __syncwarp();
+        };
+        auto values = [&](int half, int st, bool first) {
+            const uint32_t vd = v_desc + st * (OPERAND >> 4), of = tmem + half * KEYS, to = tmem + 256 + half * DIM;
+            const uint32_t more = first ? 0u : 1u;
+            if (issuer) {
+#pragma unroll
+                for (int k = 0; k < KEYS / 16; ++k) umma_f16_ts(to, of + 8 * k, desc_of(vd + k * 128, hi_desc), idesc_o, k ? 1u : more);
+            }
+            __syncwarp();
+        };
+        auto commit = [&](uint64_t *bar) {
+            if (issuer) umma_commit(bar);
+            __syncwarp();
+        };
+        int halves = 0, first = 0, last = 0;
+        auto read = [&](uint32_t it) {   // tile `it`: how many halves have queries (0: the run has ended)
+            const int slot = it % INFOS;
+            ok = mbar_wait_warp(&info_full[slot], (it / INFOS) & 1u, &abort_flag);
+            if (!ok) return 0;
+            const TileInfo &ti = info[slot];
+            const int n = ti.end < 0 ? 0 : (ti.r * ROWS + HALF < ti.m * a.G ? 2 : 1);
+            first = ti.first;
+            last = ti.last;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&info_free[slot]);
+            return n;
+        };
+        halves = read(0);
+        // The values of tile it - 1, then the scores of tile it, one half after the other.  A row tile's first scores do not wait for the results of
+        // the one before to be out, which are elsewhere in tensor memory; they come behind both halves' values, since their queries may not be there yet.
+        int before = 0;
+        bool started = false;   // tile it - 1 was a row tile's first: its values begin the sums
+        for (uint32_t it = 0; ok && (halves || before); ++it) {
+            const bool begins = halves && first, ends = last != 0;
+            const int st = it % STAGES, sv = (it + STAGES - 1) % STAGES;
+            if (halves && !begins) ok = mbar_wait_warp(&k_full[st], (it / STAGES) & 1u, &abort_flag);
+            if (ok && before) ok = mbar_wait_warp(&v_full[sv], ((it - 1) / STAGES) & 1u, &abort_flag);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                if (half >= before || !ok) break;
+                ok = mbar_wait_warp(&p_full[half], p_phase[half] & 1u, &abort_flag);
+                if (!ok) break;
+                p_phase[half] += 1;
+                tc_fence_after_sync();
+                values(half, sv, started);
+                if (half == before - 1) commit(&v_free[sv]);
+                if (halves && !begins) {
+                    scores(half, st);
+                    if (half == halves - 1) commit(&k_free[st]);
+                    if (ends) commit(&q_free[half]);
+                } else {
+                    commit(&o_done[half]);
+                }
+            }
+            if (!ok) break;
+            started = false;
+            if (begins) {
+                ok = mbar_wait_warp(&k_full[st], (it / STAGES) & 1u, &abort_flag);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    if (half >= halves || !ok) break;
+                    ok = mbar_wait_warp(&q_full[half], q_phase[half] & 1u, &abort_flag);
+                    if (!ok) break;
+                    q_phase[half] += 1;
+                    tc_fence_after_sync();
+                    scores(half, st);
+                    if (ends) commit(&q_free[half]);
+                }
+                if (!ok) break;
+                commit(&k_free[st]);
+                started = true;
+            }
+            before = halves;
+            if (halves) halves = read(it + 1);
         }
-    } else {
+    } else if (warp > FETCHER) {
+        // ---- queries ------------------------------------------------------------------------
+        // 64 rows of each half for a warp, copied as they are (all under way together); then, where bf16 rows have to be brought to fp16's range (as query_row
+        // does) or the scale is negative, whose sign goes with them, worked over in place.
+        constexpr int LANES = DIM / 8, PER = 32 / LANES, LOADS = HALF / 2 / PER;   // lanes of a row, rows of an instruction, instructions
+        const int part = lane % LANES, row_lane = (warp - FETCHER - 1) * (HALF / 2) + lane / LANES;
+        const uint32_t flip = (a.scale_log2 < 0.0f) ? 0x80008000u : 0u;
+        uint32_t uses[2] = {0, 0}, items = 0;
+        bool ok = true;
+        for (uint32_t it = 0; ok; ++it) {
+            const int slot = it % INFOS;
+            ok = mbar_wait_warp(&info_full[slot], (it / INFOS) & 1u, &abort_flag);
+            if (!ok) break;
+            const TileInfo &ti = info[slot];
+            const int end = ti.end, first = ti.first, q0 = ti.q0, rows = ti.m * a.G, r = ti.r, h = ti.h;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&info_free[slot]);
+            if (end < 0) break;
+            if (!first) continue;
+            for (int half = 0; half < 2 && ok; ++half) {
+                const int row0 = r * ROWS + half * HALF;
+                if (row0 >= rows) break;
+                ok = mbar_wait_warp(&q_free[half], (uses[half] & 1u) ^ 1u, &abort_flag);
+                if (!ok) break;
+                uses[half] += 1;
+                auto place = [&](int at) { return q_smem + half * OPERAND + (part >> 3) * PANEL + at * 128 + (((part & 7) ^ (at & 7)) << 4); };
+#pragma unroll 4
+                for (int k = 0; k < LOADS; ++k) {
+                    const int at = row_lane + k * PER, row = row0 + at, t = min(row, rows - 1) / a.G;
+                    const __half *src = static_cast<const __half *>(a.q) + (q0 + static_cast<long long>(t)) * a.q_tok + (h * a.G + min(row, rows - 1) - t * a.G) * a.q_head + part * 8;
+                    cp_async16(place(at), src, row < rows);
+                }
+                cp_async_wait_all();
+                __syncwarp();
+                if (BF16 || flip) {   // four lanes to a row
+                    constexpr int MINE = DIM / 32;   // 16-byte pieces of a lane
+#pragma unroll 1
+                    for (int k = 0; k < HALF / 2 / 8; ++k) {
+                        const int at = (warp - FETCHER - 1) * (HALF / 2) + 8 * k + (lane >> 2);
+                        uint4 *q[MINE], v[MINE];
+#pragma unroll
+                        for (int j = 0; j < MINE; ++j) {
+                            const int piece = (lane & 3) + 4 * j;   // (of 8 in a panel)
+                            q[j] = reinterpret_cast<uint4 *>(q_smem + half * OPERAND + (piece >> 3) * PANEL + at * 128 + (((piece & 7) ^ (at & 7)) << 4));
+                            v[j] = *q[j];
+                        }
+                        float g = 1.0f;
+                        if constexpr (BF16) {
+                            // the largest magnitude: bf16 magnitudes order as their bits do, two at a time
+                            uint32_t top = 0;
+#pragma unroll
+                            for (int j = 0; j < MINE; ++j) {
+                                top = __vmaxu2(top, __vmaxu2(v[j].x & 0x7fff7fffu, v[j].y & 0x7fff7fffu));
+                                top = __vmaxu2(top, __vmaxu2(v[j].z & 0x7fff7fffu, v[j].w & 0x7fff7fffu));
+                            }
+                            top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                            top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                            const int e2 = min(max(static_cast<int>(max(top >> 16, top & 0xffffu) >> 7) - 127 - 14, -100), 100);
+                            g = __uint_as_float(static_cast<uint32_t>(127 - e2) << 23);
+                            if ((lane & 3) == 0) q_exp[items & 1][half * HALF + at] = static_cast<int8_t>(e2);
+                        }
+#pragma unroll
+                        for (int j = 0; j < MINE; ++j) {
+                            uint32_t x[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                if constexpr (BF16) x[e] = half2_bits(__uint_as_float(x[e] << 16) * g, __uint_as_float(x[e] & 0xffff0000u) * g);
+                                x[e] ^= flip;
+                            }
+                            *q[j] = make_uint4(x[0], x[1], x[2], x[3]);
+                        }
+                    }
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&q_full[half]);
+            }
+            items += 1;
+        }
+    } else if (warp == FETCHER) {
         // ---- codes and scales ----------------------------------------------------------------
         Kv8Fetch<Tiles, ROWS> fetch(a, run, lane);
         uint32_t it = 0;
@@ -460,6 +552,17 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
                 }
                 // (the end, pages that are missing, and what is before a window: tiles of which some codes are not there)
                 const unsigned there = __ballot_sync(0xffffffffu, now.page >= 0);
+                if (lane == 0) {
+                    info[slot].first = now.first && t == 0;
+                    info[slot].last = now.last && t == now.tiles - 1;
+                    info[slot].tok0 = now.tok0 + t * KEYS;
+                    info[slot].q0 = now.q0;
+                    info[slot].len = now.len;
+                    info[slot].m = now.m;
+                    info[slot].r = now.r;
+                    info[slot].h = now.h;
+                    info[slot].slot = now.slot;
+                }
                 if (lane == 0) info[slot].end = (now.tok0 + (t + 1) * KEYS > now.hi || ((there >> (t * GROUPS)) & 0xffu) != 0xffu) ? 1 : 0;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&info_full[slot]);

@@ -108,6 +108,11 @@ __device__ __forceinline__ void bulk_commit_group() { asm volatile("cp.async.bul
 __device__ __forceinline__ void bulk_wait_read_all() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
+// 16 bytes global -> shared, or 16 zero bytes; both addresses 16-byte aligned.
+__device__ __forceinline__ void cp_async16(void *smem_dst, const void *src, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(smem_dst)), "l"(src), "r"(there ? 16u : 0u) : "memory");
+}
+
 // ---- tensor memory ---------------------------------------------------------------------------
 // Allocation and release are warp-wide (.sync.aligned): call with all 32 lanes of one warp.
 __device__ __forceinline__ void tmem_alloc(uint32_t *smem_result, uint32_t cols) {
