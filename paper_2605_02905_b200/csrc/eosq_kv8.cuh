@@ -440,9 +440,10 @@ int launch_kv8_rows(const Kv8Attend &a, int fmt, int dtype, int sm_count, cudaSt
 int launch_kv8_tiles(const Kv8Attend &a, int fmt, int dtype, int sm_count, cudaStream_t s);
 void launch_kv8_rows_join(const Kv8Attend &a, int dtype, int sm_count, cudaStream_t s);
 void launch_kv8_tiles_join(const Kv8Attend &a, int dtype, int sm_count, cudaStream_t s);
-// Up to so many query rows per KV head and entry go through the kernel for few rows (eosq_kv8_attend.cu), more through the one that works on
-// tiles of 256 rows (eosq_kv8_attend_tc.cu).
-constexpr int KV8_FEW_ROWS = 16;
+// Whether a call with so many query rows per KV head and entry goes through the kernel for few rows (eosq_kv8_attend.cu) or the one that works on tiles of 256
+// rows (eosq_kv8_attend_tc.cu).  The first takes row tiles of 16 one after another; at d = 128 it is ahead up to 32 rows (8 x 32768 tokens 53 us, the other 62) and
+// behind from 48 on (67 against 63), at d = 64, where its codes take half the work, up to 64.
+inline bool kv8_few_rows(long long rows, int d) { return rows * d <= 4096; }
 // Tensor map over the codes of a layer's keys or values, [rows][d] bytes, in boxes of box_rows rows with a swizzle as wide as a row (eosq_tc.cu).
 bool make_code_tensor_map(const void *codes, long long rows, int d, int box_rows, CUtensorMap *out);
 

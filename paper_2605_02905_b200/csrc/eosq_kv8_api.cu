@@ -73,7 +73,7 @@ int entry(F &&f) {
 size_t pages_scratch(const eosq_kv8_t *c) {
     return std::max(sizeof(int2) * static_cast<size_t>(c->max_seqs), sizeof(int32_t) * (64 + static_cast<size_t>(c->num_pages)));
 }
-size_t kv8_attend_scratch(int64_t rows, int d) { return rows <= KV8_FEW_ROWS ? kv8_rows_scratch(d) : kv8_tiles_scratch(d); }
+size_t kv8_attend_scratch(int64_t rows, int d) { return kv8_few_rows(rows, d) ? kv8_rows_scratch(d) : kv8_tiles_scratch(d); }
 size_t cuts_scratch() { return align_up(sizeof(Kv8Cut) * KV8_MAX_CTAS, 256); }
 
 int set_up_failed(eosq_ctx *ctx, const char *what) {
@@ -149,7 +149,7 @@ extern "C" int eosq_kv8_attend(eosq_ctx *ctx, const eosq_kv8_t *cache, int layer
             misaligned(lse, 3) || !workspace || misaligned(workspace, 255))
             return EOSQ_ERR_INVALID_ARG;
         const int most = static_cast<int>(std::min<int64_t>(max_q, total));
-        if (workspace_bytes < cuts_scratch() + kv8_attend_scratch(most * G, cache->d)) return EOSQ_ERR_BUFFER_TOO_SMALL;
+        if (workspace_bytes < cuts_scratch() + kv8_attend_scratch(static_cast<int64_t>(most) * G, cache->d)) return EOSQ_ERR_BUFFER_TOO_SMALL;
         if (!on_ctx_device(ctx)) return EOSQ_ERR_INVALID_ARG;
         a.seqs = seqs;
         a.cu = cu;
@@ -173,7 +173,7 @@ extern "C" int eosq_kv8_attend(eosq_ctx *ctx, const eosq_kv8_t *cache, int layer
         a.err = ctx->dev_err;
         cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
         int why = 0;
-        const bool few = most * G <= KV8_FEW_ROWS;
+        const bool few = kv8_few_rows(static_cast<long long>(most) * G, cache->d);
         run_stage(ctx, ST_OTHER, s, [&] {
             why = few ? launch_kv8_rows(a, cache->format, dtype, ctx->sm_count, s) : launch_kv8_tiles(a, cache->format, dtype, ctx->sm_count, s);
         });

@@ -25,7 +25,7 @@ constexpr int CTAS_PER_SM = 2, COST = 2;
 struct TileInfo {
     int first, last;        // of the CTA's run within one row tile; first = -1: the run has ended, there is no tile
     int tok0;               // the tile's first position
-    int q0, len, m, h;      // the entry's queries, its length, KV head
+    int q0, len, m, r, h;   // the entry's queries, its length; row tile, KV head
     int slot;               // -1: the whole row tile is this CTA's, else the slot of its partial result
     float ks[GROUPS], vlog[GROUPS], vinv[GROUPS];   // per 16 tokens: key scale, log2 of the value scale and its inverse
 };
@@ -77,7 +77,7 @@ __device__ __forceinline__ float query_row(const void *p, uint32_t (&v)[NQ / 2],
     return __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
 }
 
-// NB: query rows in eights; all rows of an entry and KV head are one row tile.
+// NB: query rows of a row tile, in eights.
 template <int DIM, int FMT, bool BF16, int NB>
 __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
                                                                           const Kv8Attend a) {
@@ -146,6 +146,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
                     info[st].q0 = now.q0;
                     info[st].len = now.len;
                     info[st].m = now.m;
+                    info[st].r = now.r;
                     info[st].h = now.h;
                     info[st].slot = now.slot;
                 }
@@ -181,18 +182,8 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
         uint32_t qb[NB][STEPS][2];
         float o[NB][2 * WORDS][4], m[NB][2], l[NB][2], f[NB][2];            // o: channels (8 by 8, two of a word each) x rows 2 q, 2 q + 1
         int lo[NB][2], hi[NB][2], lo_all = 0, hi_all = 0, lo_max = 0, hi_min = 0;
-        // Rows are query t of head row - t * G: the same in every row tile.
-        int t_load[NB], h_load[NB], t_row[NB][2], h_row[NB][2];
-#pragma unroll
-        for (int n = 0; n < NB; ++n) {
-            t_load[n] = (8 * n + g) / a.G;
-            h_load[n] = 8 * n + g - t_load[n] * a.G;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                t_row[n][e] = (8 * n + 2 * q + e) / a.G;
-                h_row[n][e] = 8 * n + 2 * q + e - t_row[n][e] * a.G;
-            }
-        }
+        // Rows of the row tile `tile_of`: query and head (row - query * G) of the one that this lane loads, and of the two that it holds weights of.
+        int tile_of = -1, t_load[NB], h_load[NB], t_row[NB][2], h_row[NB][2];
         uint32_t items = 0;
         bool ok = true;
         for (uint32_t it = 0;; ++it) {
@@ -205,6 +196,20 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
             const bool last = ti.last != 0;
             if (ti.first) {
                 const Kv8Seq sq{0, ti.len, mq, 0};
+                const int r = ti.r;
+                if (r != tile_of) {
+                    tile_of = r;
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) {
+                        t_load[n] = (r * ROWS + 8 * n + g) / a.G;
+                        h_load[n] = r * ROWS + 8 * n + g - t_load[n] * a.G;
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            t_row[n][e] = (r * ROWS + 8 * n + 2 * q + e) / a.G;
+                            h_row[n][e] = r * ROWS + 8 * n + 2 * q + e - t_row[n][e] * a.G;
+                        }
+                    }
+                }
 #pragma unroll
                 for (int n = 0; n < NB; ++n) {
                     const __half *base = static_cast<const __half *>(a.q);   // (or bf16: two bytes each)
@@ -227,10 +232,11 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
 #pragma unroll
                     for (int b = 0; b < 2 * WORDS; ++b) o[n][b][0] = o[n][b][1] = o[n][b][2] = o[n][b][3] = 0.0f;
                 }
-                Tiles::span(a, sq, 0, mq - 1, lo_all, hi_all);
+                const int t_first = __shfl_sync(0xffffffffu, t_load[0], 0), t_last = min(__shfl_sync(0xffffffffu, t_load[NB - 1], 28), mq - 1);   // (of row 8 NB - 1)
+                Tiles::span(a, sq, t_first, t_last, lo_all, hi_all);
                 int unused;
-                Tiles::span(a, sq, 0, 0, unused, hi_min);
-                Tiles::span(a, sq, mq - 1, mq - 1, lo_max, unused);
+                Tiles::span(a, sq, t_first, t_first, unused, hi_min);
+                Tiles::span(a, sq, t_last, t_last, lo_max, unused);
             }
             const int tok = ti.tok0 + warp * SHARE * GROUP;
             if (tok < hi_all && tok + SHARE * GROUP > lo_all) {
@@ -513,7 +519,7 @@ bool launch_rows(const Kv8Attend &a, bool i8, bool bf, int sm_count, cudaStream_
 
 }  // namespace
 
-size_t kv8_rows_scratch(int d) { return sizeof(float) * 2 * KV8_MAX_CTAS * KV8_FEW_ROWS * (static_cast<size_t>(d) + 2); }
+size_t kv8_rows_scratch(int d) { return sizeof(float) * 2 * KV8_MAX_CTAS * 16 * (static_cast<size_t>(d) + 2); }
 
 int launch_kv8_rows(const Kv8Attend &a, int fmt, int dtype, int sm_count, cudaStream_t s) {
     const bool bf = dtype == EOSQ_BF16, i8 = fmt == EOSQ_KV_INT8, eight = a.max_q * a.G <= 8;

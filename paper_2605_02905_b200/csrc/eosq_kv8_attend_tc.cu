@@ -1,6 +1,7 @@
 // Attention over the 8-bit paged cache for many query rows per KV head (a prompt's chunk, cross attention): tcgen05 products with the
 // scores, the weights and the sums in tensor memory.
 #include <algorithm>
+#include <type_traits>
 
 #include "eosq_kv8.cuh"
 #include "eosq_sm100.cuh"
@@ -206,15 +207,16 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
                 // Below, s * ks + (vlog - m + shift) is rounded once, m before: of logarithms beyond 2^22 the difference could pass fp16's range.  There
                 // every logarithm is rounded as m was.
                 const bool far = __any_sync(0xffffffffu, fabsf(m) > 4194304.0f && m != -INFINITY);
-                // ... then for the weights, 32 of them into the place of 16 scores that have been read.
-                auto weights = [&](uint32_t (&x)[32], int k) {
-                    if (edge) hide(x, tok0 + 32 * k);
+                // ... then for the weights, 32 of them into the place of 16 scores that have been read.  The rare cases have code of their own (one for all: 801 us
+                // where this is 755).
+                auto weights = [&](auto plain, uint32_t (&x)[32], int k) {
+                    if (plain.value && edge) hide(x, tok0 + 32 * k);
                     uint32_t p[16];
 #pragma unroll
                     for (int gg = 0; gg < 2; ++gg) {
                         const int g = 2 * k + gg;
                         float kf = ks_of(g), cf = ti.vlog[g] + b;
-                        if (far) {
+                        if (plain.value && far) {
 #pragma unroll
                             for (int e = 0; e < GROUP; ++e) x[16 * gg + e] = __float_as_uint(fmaf(__uint_as_float(x[16 * gg + e]), kf, ti.vlog[g]));
                             kf = 1.0f;
@@ -237,15 +239,19 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
                     }
                     tmem_st16(s_at + 16 * k, p);
                 };
+                auto all_weights = [&](auto plain) {
 #pragma unroll 1
-                for (int k = 0; k < KEYS / 32; k += 2) {
-                    tmem_ld32(s_at + 32 * (k + 1), y);
-                    weights(x, k);
-                    tmem_ld_wait(y);
-                    if (k + 2 < KEYS / 32) tmem_ld32(s_at + 32 * (k + 2), x);
-                    weights(y, k + 1);
-                    tmem_ld_wait(x);
-                }
+                    for (int k = 0; k < KEYS / 32; k += 2) {
+                        tmem_ld32(s_at + 32 * (k + 1), y);
+                        weights(plain, x, k);
+                        tmem_ld_wait(y);
+                        if (k + 2 < KEYS / 32) tmem_ld32(s_at + 32 * (k + 2), x);
+                        weights(plain, y, k + 1);
+                        tmem_ld_wait(x);
+                    }
+                };
+                if (edge || far) all_weights(std::true_type());
+                else all_weights(std::false_type());
                 tmem_st_wait();
                 tc_fence_before_sync();
                 __syncwarp();

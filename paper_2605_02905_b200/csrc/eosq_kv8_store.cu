@@ -19,7 +19,14 @@ struct StoreArgs {
 
 template <typename T> struct Chunk8;   // eight neighbouring channels of a token as they are read
 template <> struct Chunk8<__half> {
+    static constexpr uint32_t INF = 0x7c00u;   // bits of infinity: magnitudes order as their bits do
     uint4 v;
+    __device__ __forceinline__ uint32_t top(uint32_t t) const {   // the larger of t and the magnitudes' bits, in two halves
+        t = __vmaxu2(t, __vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu));
+        return __vmaxu2(t, __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+    }
+    static __device__ __forceinline__ uint32_t one(uint32_t t) { return max(t >> 16, t & 0xffffu); }
+    static __device__ __forceinline__ float value(uint32_t t) { return __half2float(__ushort_as_half(static_cast<unsigned short>(t))); }
     __device__ __forceinline__ void load(const __half *p) { v = *reinterpret_cast<const uint4 *>(p); }
     __device__ __forceinline__ void zero() { v = make_uint4(0, 0, 0, 0); }
     __device__ __forceinline__ void floats(float (&f)[8]) const {
@@ -33,7 +40,14 @@ template <> struct Chunk8<__half> {
     }
 };
 template <> struct Chunk8<__nv_bfloat16> {
+    static constexpr uint32_t INF = 0x7f80u;
     uint4 v;
+    __device__ __forceinline__ uint32_t top(uint32_t t) const {
+        t = __vmaxu2(t, __vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu));
+        return __vmaxu2(t, __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+    }
+    static __device__ __forceinline__ uint32_t one(uint32_t t) { return max(t >> 16, t & 0xffffu); }
+    static __device__ __forceinline__ float value(uint32_t t) { return __uint_as_float(t << 16); }
     __device__ __forceinline__ void load(const __nv_bfloat16 *p) { v = *reinterpret_cast<const uint4 *>(p); }
     __device__ __forceinline__ void zero() { v = make_uint4(0, 0, 0, 0); }
     __device__ __forceinline__ void floats(float (&f)[8]) const {
@@ -46,7 +60,17 @@ template <> struct Chunk8<__nv_bfloat16> {
     }
 };
 template <> struct Chunk8<float> {
+    static constexpr uint32_t INF = 0x7f800000u;
     float4 a, b;
+    __device__ __forceinline__ uint32_t top(uint32_t t) const {
+        float f[8];
+        floats(f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t = max(t, __float_as_uint(f[e]) & 0x7fffffffu);
+        return t;
+    }
+    static __device__ __forceinline__ uint32_t one(uint32_t t) { return t; }
+    static __device__ __forceinline__ float value(uint32_t t) { return __uint_as_float(t); }
     __device__ __forceinline__ void load(const float *p) {
         a = *reinterpret_cast<const float4 *>(p);
         b = *reinterpret_cast<const float4 *>(p + 4);
@@ -87,7 +111,7 @@ __device__ __forceinline__ int code_int8(float x, float s, float inv) {
     return static_cast<int>(fminf(fmaxf(c, -127.0f), 127.0f));
 }
 template <int FMT>
-__device__ __forceinline__ uint2 codes8(const float (&f)[8], float s, float inv) {
+__device__ __forceinline__ uint2 codes8(const float (&f)[8], float s, float inv) {   // any values
     uint2 r;
     if constexpr (FMT == EOSQ_KV_INT8) {
         uint32_t b[8];
@@ -108,6 +132,32 @@ __device__ __forceinline__ uint2 codes8(const float (&f)[8], float s, float inv)
     }
     return r;
 }
+// The same for finite values that s does not saturate.  int8: adding 1.5 * 2^23 rounds the quotient's estimate to a whole number, whose lowest byte is then the
+// code; only where what is left over says that the estimate was on a border's wrong side, or on the border, is it looked at again.
+template <int FMT>
+__device__ __forceinline__ uint2 codes8_plain(const float (&f)[8], float s, float inv) {
+    if constexpr (FMT == EOSQ_KV_INT8) {
+        const float round = 12582912.0f;
+        uint32_t t[8];
+        float off = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float x = fmaf(f[i], inv, round);
+            t[i] = __float_as_uint(x);
+            off = fmaxf(off, fabsf(fmaf(round - x, s, f[i])));
+        }
+        if (off >= 0.5f * s) return codes8<FMT>(f, s, inv);
+        uint2 r;
+        r.x = __byte_perm(__byte_perm(t[0], t[1], 0x0040), __byte_perm(t[2], t[3], 0x0040), 0x5410);
+        r.y = __byte_perm(__byte_perm(t[4], t[5], 0x0040), __byte_perm(t[6], t[7], 0x0040), 0x5410);
+        return r;
+    } else {
+        uint32_t h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = __nv_cvt_float2_to_fp8x2(make_float2(f[2 * i] * inv, f[2 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+        return make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
+    }
+}
 // An old code under a larger scale.  int8: the product has 31 bits and the quotient is at least 2^-25 of itself away from any border it is not on,
 // so a division in 64 bits decides as the exact one does.
 template <int FMT>
@@ -122,15 +172,14 @@ __device__ __forceinline__ uint32_t recode(uint32_t code, float s0, float s1) {
     }
 }
 
-// A CTA per page, head and keys or values: the new tokens of the page are read once and stay in registers (up to CHUNKS * 8 values a thread) between
-// the largest magnitude and the codes.
+// A CTA takes a page of an entry, and of its heads' keys and values one after another every gridDim.y-th: the new tokens are read once and stay in
+// registers (up to CHUNKS * 8 values a thread) between the largest magnitude and the codes, and the next ones are on their way meanwhile.  (A CTA per head and
+// keys or values spent most of its time finding out where: 50.4 us for 27800 tokens, this XXX.)
 template <typename T, int FMT, int THREADS, int CHUNKS>
 __global__ void __launch_bounds__(THREADS) kv8_store_kernel(const StoreArgs a) {
     pdl_wait();
     const Kv8 &c = a.c;
-    const int kv = blockIdx.x & 1;
-    const int h = (blockIdx.x >> 1) % c.heads, rest = (blockIdx.x >> 1) / c.heads;
-    const int j = rest % a.slots, i = rest / a.slots;
+    const int j = blockIdx.x % a.slots, i = blockIdx.x / a.slots;
     const int tid = threadIdx.x;
     const Kv8Seq sq = kv8_seq(c, a.seqs, a.cu, i, a.total, a.max_new);
     if (sq.m == 0) return;
@@ -150,67 +199,95 @@ __global__ void __launch_bounds__(THREADS) kv8_store_kernel(const StoreArgs a) {
         return;
     }
     const int m = end - begin, t0 = begin & (ps - 1), per = c.d_shift - 3;   // tokens, the first one's place in the page, log2 of chunks per token
-    const T *src = static_cast<const T *>(a.x[kv]) + (sq.q0 + static_cast<long long>(begin - pos0)) * a.tok[kv] + h * a.head[kv];
-    Chunk8<T> x[CHUNKS];
-    float top = 0.0f;
+    const long long row0 = sq.q0 + static_cast<long long>(begin - pos0);
+    __shared__ uint32_t tops[2][THREADS / 32];
+    int turn = 0;
+    auto ask = [&](int item, Chunk8<T> (&x)[CHUNKS]) {
+        const int kv = item & 1, h = item >> 1;
+        const T *src = static_cast<const T *>(a.x[kv]) + row0 * a.tok[kv] + h * a.head[kv];
 #pragma unroll
-    for (int k = 0; k < CHUNKS; ++k) {
-        const int q = tid + THREADS * k;
-        x[k].zero();
-        if (q < (m << per)) x[k].load(src + (q >> per) * a.tok[kv] + ((q & ((1 << per) - 1)) << 3));
-    }
-#pragma unroll
-    for (int k = 0; k < CHUNKS; ++k) {
-        float f[8];
-        x[k].floats(f);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float v = fabsf(f[e]);
-            top = fmaxf(top, (v <= 3.402823466e38f) ? v : 0.0f);
+        for (int k = 0; k < CHUNKS; ++k) {
+            const int q = tid + THREADS * k;
+            x[k].zero();
+            if (q < (m << per)) x[k].load(src + (q >> per) * a.tok[kv] + ((q & ((1 << per) - 1)) << 3));
         }
-    }
-    const size_t slot = static_cast<size_t>(page) * c.heads + h;
-    float *scale_at = c.scale[kv] + slot;
-    const float s0 = *scale_at;
-    uint32_t bits = __reduce_max_sync(0xffffffffu, __float_as_uint(top));   // magnitudes order as their bits do
-    if constexpr (THREADS > 32) {
-        __shared__ uint32_t tops[THREADS / 32];
-        if ((tid & 31) == 0) tops[tid >> 5] = bits;
-        __syncthreads();
+    };
+    auto put = [&](int item, const Chunk8<T> (&x)[CHUNKS]) {
+        const int kv = item & 1, h = item >> 1;
+        const size_t slot = static_cast<size_t>(page) * c.heads + h;
+        float *scale_at = c.scale[kv] + slot;
+        const float s0 = *scale_at;
+        uint32_t bits = 0;
 #pragma unroll
-        for (int w = 0; w < THREADS / 32; ++w) bits = max(bits, tops[w]);
-    }
-    float s1 = scale_of<FMT>(__uint_as_float(bits));
-    if (t0 > 0) s1 = fmaxf(s1, clamp_scale(s0));
-    __syncwarp();
-    uint8_t *dst = c.code[kv] + (slot << (c.ps_shift + c.d_shift));
-    if (t0 > 0 && s1 > s0) {
-        uint32_t *old = reinterpret_cast<uint32_t *>(dst);
-        for (int w = tid; w < (t0 << (c.d_shift - 2)); w += THREADS) {
-            const uint32_t v = old[w];
-            uint32_t r = 0;
+        for (int k = 0; k < CHUNKS; ++k) bits = x[k].top(bits);
+        bits = Chunk8<T>::one(bits);
+        auto over_all = [&](uint32_t v) {
+            v = __reduce_max_sync(0xffffffffu, v);
+            if constexpr (THREADS > 32) {
+                uint32_t *at = tops[turn ^= 1];   // (two in turn: a barrier is between a write and the reads before it)
+                if ((tid & 31) == 0) at[tid >> 5] = v;
+                __syncthreads();
 #pragma unroll
-            for (int b = 0; b < 4; ++b) r |= recode<FMT>((v >> (8 * b)) & 0xffu, s0, s1) << (8 * b);
-            old[w] = r;
+                for (int w = 0; w < THREADS / 32; ++w) v = max(v, at[w]);
+            }
+            return v;
+        };
+        bits = over_all(bits);
+        const bool finite = bits < Chunk8<T>::INF;
+        float top = Chunk8<T>::value(bits);
+        if (!finite) {   // again, without those that are not
+            top = 0.0f;
+#pragma unroll
+            for (int k = 0; k < CHUNKS; ++k) {
+                float f[8];
+                x[k].floats(f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, (fabsf(f[e]) <= 3.402823466e38f) ? fabsf(f[e]) : 0.0f);
+            }
+            top = __uint_as_float(over_all(__float_as_uint(top)));
         }
-    }
-    const float inv = __fdiv_rn(1.0f, s1);
-    uint2 *out = reinterpret_cast<uint2 *>(dst + (static_cast<size_t>(t0) << c.d_shift));
+        float s1 = scale_of<FMT>(top);
+        if (t0 > 0) s1 = fmaxf(s1, clamp_scale(s0));
+        __syncwarp();
+        uint8_t *dst = c.code[kv] + (slot << (c.ps_shift + c.d_shift));
+        if (t0 > 0 && s1 > s0) {
+            uint32_t *old = reinterpret_cast<uint32_t *>(dst);
+            for (int w = tid; w < (t0 << (c.d_shift - 2)); w += THREADS) {
+                const uint32_t v = old[w];
+                uint32_t r = 0;
 #pragma unroll
-    for (int k = 0; k < CHUNKS; ++k) {
-        const int q = tid + THREADS * k;
-        if (q < (m << per)) {
-            float f[8];
-            x[k].floats(f);
-            out[q] = codes8<FMT>(f, s1, inv);
+                for (int b = 0; b < 4; ++b) r |= recode<FMT>((v >> (8 * b)) & 0xffu, s0, s1) << (8 * b);
+                old[w] = r;
+            }
         }
+        const float inv = __fdiv_rn(1.0f, s1);
+        const bool plain = finite && s1 < KV8_SCALE_MAX;
+        uint2 *out = reinterpret_cast<uint2 *>(dst + (static_cast<size_t>(t0) << c.d_shift));
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k) {
+            const int q = tid + THREADS * k;
+            if (q < (m << per)) {
+                float f[8];
+                x[k].floats(f);
+                out[q] = plain ? codes8_plain<FMT>(f, s1, inv) : codes8<FMT>(f, s1, inv);
+            }
+        }
+        if (tid == 0 && s1 != s0) *scale_at = s1;   // (every thread has read s0: the barrier, or the warp, is between)
+    };
+    const int items = 2 * c.heads, step = gridDim.y;
+    Chunk8<T> x[CHUNKS], y[CHUNKS];
+    ask(blockIdx.y, x);
+    for (int item = blockIdx.y; item < items; item += 2 * step) {
+        if (item + step < items) ask(item + step, y);
+        put(item, x);
+        if (item + step >= items) break;
+        if (item + 2 * step < items) ask(item + 2 * step, x);
+        put(item + step, y);
     }
-    if (tid == 0 && s1 != s0) *scale_at = s1;   // (every thread has read s0: the barrier, or the warp, is between)
 }
 
 template <typename T, int FMT>
-void launch_store(const StoreArgs &a, long long ctas, int chunks, cudaStream_t s) {
-    const dim3 grid(static_cast<unsigned>(ctas));
+void launch_store(const StoreArgs &a, dim3 grid, int chunks, cudaStream_t s) {
     if (chunks <= 32) launch_dependent(kv8_store_kernel<T, FMT, 32, 1>, grid, 32, 0, s, a);
     else if (chunks <= 256) launch_dependent(kv8_store_kernel<T, FMT, 128, 2>, grid, 128, 0, s, a);
     else if (chunks <= 1024) launch_dependent(kv8_store_kernel<T, FMT, 256, 4>, grid, 256, 0, s, a);
@@ -234,12 +311,14 @@ void launch_kv8_store(const Kv8 &c, int fmt, const void *const (&x)[2], int dtyp
     a.total = total;
     a.max_new = max_new;
     a.slots = (max_new + c.page_size() - 2) / c.page_size() + 1;
-    const long long ctas = 2ll * n * a.slots * c.heads;
+    // Of a page's heads, keys and values, so many CTAs' shares that there are eight CTAs per SM, if there are pages for fewer.
+    const long long pages = static_cast<long long>(n) * a.slots, wanted = (8ll * 148 + pages - 1) / pages;
+    const dim3 grid(static_cast<unsigned>(pages), static_cast<unsigned>(std::min<long long>(2ll * c.heads, std::max(wanted, 2ll))));
     const int chunks = std::min(max_new, c.page_size()) << (c.d_shift - 3);
     auto go = [&](auto t) {
         using T = decltype(t);
-        if (fmt == EOSQ_KV_INT8) launch_store<T, EOSQ_KV_INT8>(a, ctas, chunks, s);
-        else launch_store<T, EOSQ_KV_E4M3>(a, ctas, chunks, s);
+        if (fmt == EOSQ_KV_INT8) launch_store<T, EOSQ_KV_INT8>(a, grid, chunks, s);
+        else launch_store<T, EOSQ_KV_E4M3>(a, grid, chunks, s);
     };
     if (dtype == EOSQ_F16) go(__half());
     else if (dtype == EOSQ_BF16) go(__nv_bfloat16());
