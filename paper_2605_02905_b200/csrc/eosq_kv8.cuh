@@ -23,6 +23,24 @@ struct Kv8 {
     __host__ __device__ size_t page_bytes() const { return static_cast<size_t>(heads) << (ps_shift + d_shift); }   // of keys, or of values
 };
 
+// ---- two numbers in an instruction ----------------------------------------------------------------
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t p, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p)); }
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 // ---- codes ------------------------------------------------------------------------------------
 constexpr float KV8_SCALE_MIN = 5.421010862427522e-20f;   // 2^-64
 constexpr float KV8_SCALE_MAX = 1.8446744073709552e19f;   // 2^64

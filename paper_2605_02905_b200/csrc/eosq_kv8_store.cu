@@ -137,14 +137,18 @@ __device__ __forceinline__ uint2 codes8(const float (&f)[8], float s, float inv)
 template <int FMT>
 __device__ __forceinline__ uint2 codes8_plain(const float (&f)[8], float s, float inv) {
     if constexpr (FMT == EOSQ_KV_INT8) {
-        const float round = 12582912.0f;
+        const uint64_t round = pair_of(12582912.0f, 12582912.0f), back = pair_of(-12582912.0f, -12582912.0f), by = pair_of(inv, inv), less = pair_of(-s, -s);
         uint32_t t[8];
         float off = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float x = fmaf(f[i], inv, round);
-            t[i] = __float_as_uint(x);
-            off = fmaxf(off, fabsf(fmaf(round - x, s, f[i])));
+        for (int i = 0; i < 8; i += 2) {
+            const uint64_t y = pair_of(f[i], f[i + 1]), x = fma_pair(y, by, round);
+            float lo, hi;
+            unpair(fma_pair(add_pair(x, back), less, y), lo, hi);
+            off = fmaxf(off, fmaxf(fabsf(lo), fabsf(hi)));
+            unpair(x, lo, hi);
+            t[i] = __float_as_uint(lo);
+            t[i + 1] = __float_as_uint(hi);
         }
         if (off >= 0.5f * s) return codes8<FMT>(f, s, inv);
         uint2 r;
@@ -174,7 +178,7 @@ __device__ __forceinline__ uint32_t recode(uint32_t code, float s0, float s1) {
 
 // A CTA takes a page of an entry, and of its heads' keys and values one after another every gridDim.y-th: the new tokens are read once and stay in
 // registers (up to CHUNKS * 8 values a thread) between the largest magnitude and the codes, and the next ones are on their way meanwhile.  (A CTA per head and
-// keys or values spent most of its time finding out where: 50.4 us for 27800 tokens, this XXX.)
+// keys or values spent most of its time finding out where: 50.4 us for 27800 tokens, this 35.)
 template <typename T, int FMT, int THREADS, int CHUNKS>
 __global__ void __launch_bounds__(THREADS) kv8_store_kernel(const StoreArgs a) {
     pdl_wait();
@@ -202,8 +206,9 @@ __global__ void __launch_bounds__(THREADS) kv8_store_kernel(const StoreArgs a) {
     const long long row0 = sq.q0 + static_cast<long long>(begin - pos0);
     __shared__ uint32_t tops[2][THREADS / 32];
     int turn = 0;
-    auto ask = [&](int item, Chunk8<T> (&x)[CHUNKS]) {
+    auto ask = [&](int item, Chunk8<T> (&x)[CHUNKS], float &s0) {
         const int kv = item & 1, h = item >> 1;
+        if (t0 > 0) s0 = c.scale[kv][static_cast<size_t>(page) * c.heads + h];   // (a page that begins here has none yet)
         const T *src = static_cast<const T *>(a.x[kv]) + row0 * a.tok[kv] + h * a.head[kv];
 #pragma unroll
         for (int k = 0; k < CHUNKS; ++k) {
@@ -212,11 +217,9 @@ __global__ void __launch_bounds__(THREADS) kv8_store_kernel(const StoreArgs a) {
             if (q < (m << per)) x[k].load(src + (q >> per) * a.tok[kv] + ((q & ((1 << per) - 1)) << 3));
         }
     };
-    auto put = [&](int item, const Chunk8<T> (&x)[CHUNKS]) {
+    auto put = [&](int item, const Chunk8<T> (&x)[CHUNKS], float s0) {
         const int kv = item & 1, h = item >> 1;
         const size_t slot = static_cast<size_t>(page) * c.heads + h;
-        float *scale_at = c.scale[kv] + slot;
-        const float s0 = *scale_at;
         uint32_t bits = 0;
 #pragma unroll
         for (int k = 0; k < CHUNKS; ++k) bits = x[k].top(bits);
@@ -248,7 +251,6 @@ __global__ void __launch_bounds__(THREADS) kv8_store_kernel(const StoreArgs a) {
         }
         float s1 = scale_of<FMT>(top);
         if (t0 > 0) s1 = fmaxf(s1, clamp_scale(s0));
-        __syncwarp();
         uint8_t *dst = c.code[kv] + (slot << (c.ps_shift + c.d_shift));
         if (t0 > 0 && s1 > s0) {
             uint32_t *old = reinterpret_cast<uint32_t *>(dst);
@@ -272,17 +274,18 @@ __global__ void __launch_bounds__(THREADS) kv8_store_kernel(const StoreArgs a) {
                 out[q] = plain ? codes8_plain<FMT>(f, s1, inv) : codes8<FMT>(f, s1, inv);
             }
         }
-        if (tid == 0 && s1 != s0) *scale_at = s1;   // (every thread has read s0: the barrier, or the warp, is between)
+        if (tid == 0) c.scale[kv][slot] = s1;   // (every thread has its s0: the reduction has been between)
     };
     const int items = 2 * c.heads, step = gridDim.y;
     Chunk8<T> x[CHUNKS], y[CHUNKS];
-    ask(blockIdx.y, x);
+    float sx = 0.0f, sy = 0.0f;
+    ask(blockIdx.y, x, sx);
     for (int item = blockIdx.y; item < items; item += 2 * step) {
-        if (item + step < items) ask(item + step, y);
-        put(item, x);
+        if (item + step < items) ask(item + step, y, sy);
+        put(item, x, sx);
         if (item + step >= items) break;
-        if (item + 2 * step < items) ask(item + 2 * step, x);
-        put(item + step, y);
+        if (item + 2 * step < items) ask(item + 2 * step, x, sx);
+        put(item + step, y, sy);
     }
 }
 
@@ -290,8 +293,9 @@ template <typename T, int FMT>
 void launch_store(const StoreArgs &a, dim3 grid, int chunks, cudaStream_t s) {
     if (chunks <= 32) launch_dependent(kv8_store_kernel<T, FMT, 32, 1>, grid, 32, 0, s, a);
     else if (chunks <= 256) launch_dependent(kv8_store_kernel<T, FMT, 128, 2>, grid, 128, 0, s, a);
+    else if (chunks <= 512) launch_dependent(kv8_store_kernel<T, FMT, 128, 4>, grid, 128, 0, s, a);
     else if (chunks <= 1024) launch_dependent(kv8_store_kernel<T, FMT, 256, 4>, grid, 256, 0, s, a);
-    else launch_dependent(kv8_store_kernel<T, FMT, 256, 8>, grid, 256, 0, s, a);
+    else launch_dependent(kv8_store_kernel<T, FMT, 512, 4>, grid, 512, 0, s, a);
 }
 
 }  // namespace
