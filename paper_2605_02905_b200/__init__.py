@@ -382,6 +382,9 @@ def eosq_check_status(ctx: Context, cache: Cache, stream=None) -> int:
 # These calls are a serving loop's, one per layer and token, so what surrounds the C call is kept short: sizes that follow from the cache are worked
 # out with the handle, tensors are checked by single attributes, and the stream is asked for as a number.
 
+_torch = None   # set by the first Kv8Cache: an import statement in every call would cost as much as one of its checks
+
+
 class Kv8Cache:
     """``eosq_kv8_t`` over torch tensors: keys and values of the tokens that no compressed block holds, a byte per number, in
     pages that sequences own through a table in device memory.
@@ -394,7 +397,9 @@ class Kv8Cache:
                  "page_size", "d", "max_seqs", "max_pages", "device", "_struct", "_address", "_index", "_scratch", "_scale")
 
     def __init__(self, *, k, v, k_scale, v_scale, table, lengths, refs, format, flags=None):
+        global _torch
         import torch
+        _torch = torch
         if k.dim() != 5 or table.dim() != 2:
             raise ValueError("k is [layers][num_pages][kv_heads][page_size][d], table [max_seqs][max_pages]")
         layers, num_pages, kv_heads, page_size, d = k.shape
@@ -437,8 +442,7 @@ class Kv8Cache:
 
 
 def _kv8_list(cache, t, n, what):
-    import torch
-    if t.dtype is not torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.get_device() != cache._index or (n is not None and t.shape[0] != n):
+    if t.dtype is not _torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.get_device() != cache._index or (n is not None and t.size(0) != n):
         raise ValueError(f"{what}: int32 [{n if n is not None else 'n'}] contiguous on {cache.device} is wanted, not {t.dtype} {list(t.shape)} on {t.device}")
     return t.data_ptr()
 
@@ -452,34 +456,30 @@ def _kv8_rows(cache, t, heads, what):
 
 
 def _any_dtype_code(t):
-    import torch
-    return EOSQ_BF16 if t.dtype is torch.bfloat16 else _dtype_code(t)
+    return EOSQ_BF16 if t.dtype is _torch.bfloat16 else _dtype_code(t)
 
 
 def _kv8_stream(cache, stream):
-    import torch
-    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(cache._index)
+    return stream.cuda_stream if stream is not None else _torch._C._cuda_getCurrentRawStream(cache._index)
 
 
 def _new(like, shape, dtype, stream):
     """Memory on `like`'s device that belongs to the stream it is used on: freed, it goes back to that stream's later work."""
-    import torch
     if stream is None:
-        return like.new_empty(shape, dtype=dtype)
-    with torch.cuda.stream(stream):
+        return like.new_empty(shape) if like.dtype is dtype else like.new_empty(shape, dtype=dtype)
+    with _torch.cuda.stream(stream):
         return like.new_empty(shape, dtype=dtype)
 
 
 def _kv8_workspace(cache, rows, workspace, stream):
     """(tensor, address, bytes)"""
-    import torch
     if workspace is None:
         need = cache._scratch.get(rows)
         if need is None:
             if len(cache._scratch) > 64:
                 cache._scratch.clear()
             need = cache._scratch[rows] = max(eosq_kv8_workspace_bytes(cache, rows), 256)
-        workspace = _new(cache.k, need, torch.uint8, stream)
+        workspace = _new(cache.k, need, _torch.uint8, stream)
         return workspace, workspace.data_ptr(), need
     if workspace.get_device() != cache._index or not workspace.is_contiguous():
         raise ValueError(f"workspace: contiguous memory on {cache.device} is wanted")
@@ -492,10 +492,9 @@ def eosq_kv8_workspace_bytes(cache: Kv8Cache, query_rows: int = 0) -> int:
 
 def eosq_kv8_reserve(ctx: Context, cache: Kv8Cache, seqs, add, first=None, stream=None):
     """Room for add[i] more tokens of sequence seqs[i].  Returns the position of each one's first new token, -1 where refused."""
-    import torch
     n = seqs.shape[0]
     if first is None:
-        first = _new(seqs, n, torch.int32, stream)
+        first = _new(seqs, n, _torch.int32, stream)
     rc = lib().eosq_kv8_reserve(ctx._h, cache._address, _kv8_list(cache, seqs, None, "seqs"), _kv8_list(cache, add, n, "add"), n,
                                 _kv8_list(cache, first, n, "first"), _kv8_stream(cache, stream))
     _check(rc, "eosq_kv8_reserve", ctx)
@@ -517,20 +516,22 @@ def eosq_kv8_store(ctx: Context, cache: Kv8Cache, layer: int, k, v, seqs, first,
 def eosq_kv8_attend(ctx: Context, cache: Kv8Cache, layer: int, q, seqs, cu, max_q: int, scale: Optional[float] = None, causal: bool = True,
                     window: int = 0, out=None, lse=None, want_lse: bool = False, workspace=None, stream=None):
     """q: [total][kv_heads * G][d] fp16 or bf16.  Returns out, or (out, lse) with want_lse (or with an lse to write to)."""
-    import torch
-    n, total, H = seqs.shape[0], q.shape[0], q.shape[1]
+    n = seqs.size(0)
+    total, H = q.shape[0], q.shape[1]
     if H % cache.kv_heads or H == 0:
         raise ValueError(f"q has {H} heads, not a multiple of {cache.kv_heads}")
     G = H // cache.kv_heads
     qp, qt, qh = _kv8_rows(cache, q, H, "q")
     if out is None:
-        out = _new(q, (total, H, cache.d), q.dtype, stream)
-    elif out.dtype is not q.dtype or out.shape[0] != total:
-        raise ValueError(f"out: {q.dtype} [{total}][{H}][{cache.d}] is wanted")
-    op, ot, oh = _kv8_rows(cache, out, H, "out")
+        out = _torch.empty_like(q) if stream is None and q.is_contiguous() else _new(q, (total, H, cache.d), q.dtype, stream)
+        op, ot, oh = out.data_ptr(), H * cache.d, cache.d
+    else:
+        if out.dtype is not q.dtype or out.shape[0] != total:
+            raise ValueError(f"out: {q.dtype} [{total}][{H}][{cache.d}] is wanted")
+        op, ot, oh = _kv8_rows(cache, out, H, "out")
     if want_lse and lse is None:
-        lse = _new(q, (total, H), torch.float32, stream)
-    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (total, H) or not lse.is_contiguous() or lse.device != cache.device):
+        lse = _new(q, (total, H), _torch.float32, stream)
+    if lse is not None and (lse.dtype != _torch.float32 or tuple(lse.shape) != (total, H) or not lse.is_contiguous() or lse.device != cache.device):
         raise ValueError(f"lse: float32 [{total}][{H}] contiguous on {cache.device} is wanted")
     workspace, ws, ws_bytes = _kv8_workspace(cache, min(max_q, total) * G, workspace, stream)
     if scale is None:
@@ -557,9 +558,8 @@ def eosq_kv8_free(ctx: Context, cache: Kv8Cache, seqs, stream=None) -> None:
 
 def eosq_kv8_compact(ctx: Context, cache: Kv8Cache, remap=None, workspace=None, stream=None):
     """Moves the used pages to the front of the pool.  Returns where each page went, -1 for one that was free."""
-    import torch
     if remap is None:
-        remap = _new(cache.refs, cache.num_pages, torch.int32, stream)
+        remap = _new(cache.refs, cache.num_pages, _torch.int32, stream)
     workspace, ws, ws_bytes = _kv8_workspace(cache, 0, workspace, stream)
     rc = lib().eosq_kv8_compact(ctx._h, cache._address, _kv8_list(cache, remap, cache.num_pages, "remap"), ws, ws_bytes, _kv8_stream(cache, stream))
     _check(rc, "eosq_kv8_compact", ctx)

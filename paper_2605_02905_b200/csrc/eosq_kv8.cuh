@@ -368,16 +368,19 @@ __device__ __forceinline__ float row_lse(float m, float l) {
     return (m - KV8_SHIFT + log2f(l)) * 0.6931471805599453f;
 }
 
-// Partial results: [slots][ROWS][d] sums, then [slots][ROWS] maxima, then sums of weights.
+// Partial results: sums as [slots][d / 4][RT][4], so that neighbouring rows' go side by side, then [slots][RT] maxima, then sums of weights.
 template <int RT>
 struct Kv8Parts {
     float *o, *m, *l;
-    __device__ __forceinline__ Kv8Parts(const Kv8Attend &a, int ctas) {
+    int d_shift;
+    __device__ __forceinline__ Kv8Parts(const Kv8Attend &a, int ctas) : d_shift(a.c.d_shift) {
         const size_t rows = static_cast<size_t>(2) * ctas * RT;
         o = a.part;
-        m = o + (rows << a.c.d_shift);
+        m = o + (rows << d_shift);
         l = m + rows;
     }
+    // Four channels from `ch` on (a multiple of four).
+    __device__ __forceinline__ float *four(int slot, int row, int ch) const { return o + (((static_cast<size_t>(slot) << (d_shift - 2)) + (ch >> 2)) * RT + row) * 4; }
 };
 
 // What a CTA says about its last row tile: whether it goes on behind the run [.., u1) of `ctas` runs.
@@ -400,9 +403,9 @@ __global__ void __launch_bounds__(128) kv8_join_kernel(const Kv8Attend a, int ct
     if (cut.last_cta < 0 || cut.r * RT + row0 >= rows) return;
     const Kv8Parts<RT> parts(a, ctas);
     constexpr int PART = 8, LANES = DIM / PART;   // threads per row
-    for (int row = row0 + threadIdx.x / LANES; row < row0 + JOIN; row += 128 / LANES) {
-        const int at = cut.r * RT + row, part = threadIdx.x % LANES;
-        if (at >= rows) break;
+    for (int i = threadIdx.x; i < JOIN * LANES; i += 128) {
+        const int row = row0 + i % JOIN, at = cut.r * RT + row, part = i / JOIN;
+        if (at >= rows) continue;
         float top = -INFINITY;
         for (int k = ca; k <= cut.last_cta; ++k) top = fmaxf(top, parts.m[static_cast<size_t>(2 * k + (k == ca)) * RT + row]);
         float l = 0.0f, v[PART];
@@ -412,8 +415,8 @@ __global__ void __launch_bounds__(128) kv8_join_kernel(const Kv8Attend a, int ct
             const size_t pr = static_cast<size_t>(2 * k + (k == ca)) * RT + row;
             const float mk = parts.m[pr], f = (mk == -INFINITY) ? 0.0f : exp2_fast(mk - top);
             l = fmaf(parts.l[pr], f, l);
-            const float4 x = *reinterpret_cast<const float4 *>(parts.o + pr * DIM + part * PART);
-            const float4 y = *reinterpret_cast<const float4 *>(parts.o + pr * DIM + part * PART + 4);
+            const float4 x = *reinterpret_cast<const float4 *>(parts.four(2 * k + (k == ca), row, part * PART));
+            const float4 y = *reinterpret_cast<const float4 *>(parts.four(2 * k + (k == ca), row, part * PART + 4));
             v[0] = fmaf(x.x, f, v[0]); v[1] = fmaf(x.y, f, v[1]); v[2] = fmaf(x.z, f, v[2]); v[3] = fmaf(x.w, f, v[3]);
             v[4] = fmaf(y.x, f, v[4]); v[5] = fmaf(y.y, f, v[5]); v[6] = fmaf(y.z, f, v[6]); v[7] = fmaf(y.w, f, v[7]);
         }

@@ -478,7 +478,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
                         const Kv8Parts<ROWS> parts(a, gridDim.x);
                         const size_t pr = static_cast<size_t>(2 * blockIdx.x + slot) * ROWS + row;
 #pragma unroll
-                        for (int b = 0; b < QUARTER; ++b) *reinterpret_cast<float2 *>(parts.o + pr * DIM + ch + 2 * b) = make_float2(x[n][b][e], x[n][b][2 + e]);
+                        for (int b = 0; b < QUARTER; ++b) *reinterpret_cast<float2 *>(parts.four(2 * blockIdx.x + slot, row, (ch + 2 * b) & ~3) + ((ch + 2 * b) & 3)) = make_float2(x[n][b][e], x[n][b][2 + e]);
                         if (warp == 0 && g == 0) {
                             parts.m[pr] = top[n][e];
                             parts.l[pr] = total[n][e];

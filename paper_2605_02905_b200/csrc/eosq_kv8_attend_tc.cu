@@ -19,7 +19,9 @@ namespace {
 //   warp 12          issues the products; while one half's weights are made, the other half's products run
 //   warp 13          walks through the run, tells the others about each tile, and fetches codes, a tile ahead, and scales
 //   warps 14, 15     bring the next row tile's queries in as soon as this one's last scores have been made
-// The weights are the bottleneck: 2^x of 128 x 256 scores is 2048 cycles of an SM's special function units, as many as the two products take.
+// A half's chain is what bounds it: products of 128 x 128 x d twice (some 1500 cycles, shared memory feeding them), then the weights of a row per thread (some 2500, of
+// which the special function units need 1024, or 2048 where the halves meet); the halves overlap, so a tile takes some 4400 cycles.  Half the weights' 2^x by a polynomial
+// instead was slower, so were scores of 64 tokens with the next 64 beside them, and twice the warps for the codes.
 constexpr int ROWS = 256, HALF = 128, KEYS = KV8_KEYS, GROUP = KV8_GROUP, GROUPS = KV8_GROUPS;
 constexpr int LOADER = 8, ISSUER = 12, FETCHER = 13, THREADS = 32 * 16, STAGES = 2, INFOS = 4;
 constexpr int COST = 2;
@@ -120,7 +122,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
                 const int row0 = ti.r * ROWS + half * HALF, rows = ti.m * a.G;
                 active = row0 < rows;
                 live = row0 + row_in < rows;
-                lo = hi = 0;
+                lo = 0;
+                hi = 1 << 30;   // (rows that are no query see everything: that they saw nothing would hold up the others)
                 if (live) {
                     const int t = (row0 + row_in) / a.G;
                     Tiles::span(a, Kv8Seq{0, ti.len, ti.m, 0}, t, t, lo, hi);
@@ -137,104 +140,140 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
                 tc_fence_after_sync();
                 if (BF16 && first) kscale = scale * __uint_as_float(static_cast<uint32_t>(127 + q_exp[items & 1][half * HALF + row_in]) << 23);
                 // A row's base-2 logarithms are s * ks + vlog, with a key and a value scale for every 16 tokens.  (ks is kept above zero, so that masked scores stay
-                // -infinity under a scale of zero.)  The scores are read twice, 32 at a time: all 128 in registers, in straight code, took longer.  First the largest, ...
+                // -infinity under a scale of zero.)
                 auto ks_of = [&](int g) { return fmaxf(ti.ks[g] * kscale, 1e-37f); };
-                auto hide = [&](uint32_t (&x)[32], int at) {
+                uint32_t x[GROUP];
+                auto read = [&](int g) {
+                    tmem_ld16(s_at + GROUP * g, x);
+                    tmem_ld_wait(x);
+                };
+                auto hide = [&](int g) {
+                    const int at = tok0 + GROUP * g;
 #pragma unroll
-                    for (int e = 0; e < 32; ++e)
+                    for (int e = 0; e < GROUP; ++e)
                         if (at + e < lo || at + e >= hi) x[e] = 0xff800000u;   // -infinity
                 };
-                float top = -INFINITY;
-                auto largest = [&](uint32_t (&x)[32], int k) {
-                    if (edge) hide(x, tok0 + 32 * k);
+                // The largest logarithm of the 16 tokens in x ...
+                auto largest = [&](int g) {
+                    float t0 = __uint_as_float(x[0]), t1 = __uint_as_float(x[1]);
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) {
-                        float t0 = __uint_as_float(x[16 * g]), t1 = __uint_as_float(x[16 * g + 1]);
-#pragma unroll
-                        for (int e = 2; e < GROUP; e += 2) {
-                            t0 = fmaxf(t0, __uint_as_float(x[16 * g + e]));
-                            t1 = fmaxf(t1, __uint_as_float(x[16 * g + e + 1]));
-                        }
-                        top = fmaxf(top, fmaf(fmaxf(t0, t1), ks_of(2 * k + g), ti.vlog[2 * k + g]));
+                    for (int e = 2; e < GROUP; e += 2) {
+                        t0 = fmaxf(t0, __uint_as_float(x[e]));
+                        t1 = fmaxf(t1, __uint_as_float(x[e + 1]));
                     }
+                    return fmaf(fmaxf(t0, t1), ks_of(g), ti.vlog[g]);
                 };
-                uint32_t x[32], y[32];
-                tmem_ld32(s_at, x);
-                tmem_ld_wait(x);
-#pragma unroll 1
-                for (int k = 0; k < KEYS / 32; k += 2) {
-                    tmem_ld32(s_at + 32 * (k + 1), y);
-                    largest(x, k);
-                    tmem_ld_wait(y);
-                    tmem_ld32(s_at + 32 * ((k + 2) % (KEYS / 32)), x);   // (at the end the first ones again)
-                    largest(y, k + 1);
-                    tmem_ld_wait(x);
-                }
-                if (__any_sync(0xffffffffu, top > m + KV8_SLACK)) {
-                    const float n = fmaxf(m, top), by = (n == -INFINITY) ? 1.0f : exp2_fast(m - n);
-                    m = n;
+                // ... their weights, as 2^(x * kf + cf), and the sum of those.
+                uint32_t p[GROUP / 2];
+                auto weights = [&](const uint32_t (&x)[GROUP], uint32_t (&p)[GROUP / 2], float kf, float cf) {
+                    const uint64_t k2 = pair_of(kf, kf), c2 = pair_of(cf, cf);
+                    uint64_t sum = 0;
+#pragma unroll
+                    for (int e = 0; e < GROUP; e += 2) {
+                        float y0, y1;
+                        unpair(fma_pair(pair_of(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), k2, c2), y0, y1);
+                        y0 = exp2_fast(y0);
+                        y1 = exp2_fast(y1);
+                        sum = add_pair(sum, pair_of(y0, y1));
+                        p[e >> 1] = half2_bits(y0, y1);
+                    }
+                    float s0, s1;
+                    unpair(sum, s0, s1);
+                    return s0 + s1;
+                };
+                // A new maximum, for the sum and for the sums of values (the products that made them have ended: the scores came behind them).  A maximum only moves up,
+                // by whole powers of two, so that what has been rounded already is rescaled exactly.
+                auto move = [&](float top) {
+                    const float to = (m == -INFINITY) ? top : m + ceilf(fmaxf(top - m, 0.0f)), by = (to == -INFINITY) ? 1.0f : exp2_fast(m - to);
+                    m = to;
                     l *= by;
-                    if (!first) {   // the sums so far: the products that made them have ended, the scores came behind them
+                    if (!first) {
 #pragma unroll 1
-                        for (int k = 0; k < DIM / 32; ++k) {
-                            uint32_t o[32];
-                            tmem_ld32(o_at + 32 * k, o);
-                            tmem_ld_wait(o);
+                        for (int k = 0; k < DIM / 16; ++k) {
+                            tmem_ld16(o_at + 16 * k, x);
+                            tmem_ld_wait(x);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
-                            tmem_st32(o_at + 32 * k, o);
+                            for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * by);
+                            tmem_st16(o_at + 16 * k, x);
                         }
+                    }
+                    return by;
+                };
+                // Short loops: the warps of a quarter of an SM all run different parts of this kernel through one small instruction cache.  And one pass over the scores
+                // where it can be.  Four prompts of 500 to 2048 queries on up to 12000 tokens, and four of 2048 on 12000: two passes in loops of 32 tokens, twice unrolled,
+                // 745 and 1879 us; of 16 tokens 635 and 1687; one pass of 16 tokens 638 and 1662, of 32 634 and 1524, of 64 629 and 1458.
+                constexpr int TURN = 4;   // in sixteens
+                if (first || edge || __any_sync(0xffffffffu, m == -INFINITY || fabsf(m) > 4194304.0f)) {
+                    // With a look at all scores before the first weight: a row tile's first tile, masks, rows that have seen nothing yet; and logarithms so large that
+                    // s * ks + (vlog - m + shift), which is rounded once, could pass fp16's range where m was rounded before: there every one is rounded as m was.
+                    float top = -INFINITY;
+#pragma unroll 1
+                    for (int g = 0; g < GROUPS; ++g) {
+                        read(g);
+                        if (edge) hide(g);
+                        top = fmaxf(top, largest(g));
+                    }
+                    if (__any_sync(0xffffffffu, top > m + KV8_SLACK)) move(top);
+                    const bool far = __any_sync(0xffffffffu, fabsf(m) > 4194304.0f && m != -INFINITY);
+                    const float b = (m == -INFINITY) ? 0.0f : KV8_SHIFT - m;
+#pragma unroll 1
+                    for (int g = 0; g < GROUPS; ++g) {
+                        read(g);
+                        if (edge) hide(g);
+                        float kf = ks_of(g), cf = ti.vlog[g];
+                        if (far) {
+#pragma unroll
+                            for (int e = 0; e < GROUP; ++e) x[e] = __float_as_uint(fmaf(__uint_as_float(x[e]), kf, cf));
+                            kf = 1.0f;
+                            cf = 0.0f;
+                        }
+                        l = fmaf(weights(x, p, kf, cf + b), ti.vinv[g], l);
+                        tmem_st8(s_at + GROUP / 2 * g, p);   // in the place of scores that have been read
+                    }
+                } else {
+                    // Under the maximum so far.  Where the weights of a turn add up to no more than 2^14 none is beyond fp16's range, nor is the maximum more than KV8_SLACK behind; else, which
+                    // is rare, it is moved and they are made again.
+#pragma unroll 1
+                    for (int g = 0; g < GROUPS; g += TURN) {
+                        uint32_t y[TURN][GROUP], q[TURN][GROUP / 2];
+#pragma unroll
+                        for (int i = 0; i < TURN; ++i) tmem_ld16(s_at + GROUP * (g + i), y[i]);
+                        float sum = 0.0f, add = 0.0f;
+#pragma unroll
+                        for (int i = 0; i < TURN; ++i) {
+                            const float kf = ks_of(g + i), cf = ti.vlog[g + i] + KV8_SHIFT;
+                            tmem_ld_wait(y[i]);
+                            const float s16 = weights(y[i], q[i], kf, cf - m);
+                            sum += s16;
+                            add = fmaf(s16, ti.vinv[g + i], add);
+                        }
+                        if (__any_sync(0xffffffffu, sum > 16384.0f)) {   // (not for a NaN, which stays one)
+                            float top = -INFINITY;
+#pragma unroll 1
+                            for (int i = g; i < g + TURN; ++i) {
+                                read(i);
+                                top = fmaxf(top, largest(i));
+                            }
+                            const __half2 by = __float2half2_rn(move(top));
+#pragma unroll 1
+                            for (int i = 0; i < g; ++i) {   // the weights before these
+                                tmem_ld8(s_at + GROUP / 2 * i, p);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int e = 0; e < GROUP / 2; ++e) {
+                                    const __half2 v = __hmul2(*reinterpret_cast<const __half2 *>(&p[e]), by);
+                                    p[e] = *reinterpret_cast<const uint32_t *>(&v);
+                                }
+                                tmem_st8(s_at + GROUP / 2 * i, p);
+                            }
+                            g -= TURN;
+                            continue;
+                        }
+                        l += add;
+#pragma unroll
+                        for (int i = 0; i < TURN; ++i) tmem_st8(s_at + GROUP / 2 * (g + i), q[i]);   // in the place of scores that have been read
                     }
                 }
-                const float b = (m == -INFINITY) ? 0.0f : KV8_SHIFT - m;
-                // Below, s * ks + (vlog - m + shift) is rounded once, m before: of logarithms beyond 2^22 the difference could pass fp16's range.  There
-                // every logarithm is rounded as m was.
-                const bool far = __any_sync(0xffffffffu, fabsf(m) > 4194304.0f && m != -INFINITY);
-                // ... then for the weights, 32 of them into the place of 16 scores that have been read.  The rare cases have code of their own (one for all: 801 us
-                // where this is 755).
-                auto weights = [&](auto plain, uint32_t (&x)[32], int k) {
-                    if (plain.value && edge) hide(x, tok0 + 32 * k);
-                    uint32_t p[16];
-#pragma unroll
-                    for (int gg = 0; gg < 2; ++gg) {
-                        const int g = 2 * k + gg;
-                        float kf = ks_of(g), cf = ti.vlog[g] + b;
-                        if (plain.value && far) {
-#pragma unroll
-                            for (int e = 0; e < GROUP; ++e) x[16 * gg + e] = __float_as_uint(fmaf(__uint_as_float(x[16 * gg + e]), kf, ti.vlog[g]));
-                            kf = 1.0f;
-                            cf = b;
-                        }
-                        const uint64_t k2 = pair_of(kf, kf), c2 = pair_of(cf, cf);
-                        uint64_t sum = 0;
-#pragma unroll
-                        for (int e = 0; e < GROUP; e += 2) {
-                            float y0, y1;
-                            unpair(fma_pair(pair_of(__uint_as_float(x[16 * gg + e]), __uint_as_float(x[16 * gg + e + 1])), k2, c2), y0, y1);
-                            y0 = exp2_fast(y0);
-                            y1 = exp2_fast(y1);
-                            sum = add_pair(sum, pair_of(y0, y1));
-                            p[8 * gg + (e >> 1)] = half2_bits(y0, y1);
-                        }
-                        float s0, s1;
-                        unpair(sum, s0, s1);
-                        l = fmaf(s0 + s1, ti.vinv[g], l);
-                    }
-                    tmem_st16(s_at + 16 * k, p);
-                };
-                auto all_weights = [&](auto plain) {
-#pragma unroll 1
-                    for (int k = 0; k < KEYS / 32; k += 2) {
-                        tmem_ld32(s_at + 32 * (k + 1), y);
-                        weights(plain, x, k);
-                        tmem_ld_wait(y);
-                        if (k + 2 < KEYS / 32) tmem_ld32(s_at + 32 * (k + 2), x);
-                        weights(plain, y, k + 1);
-                        tmem_ld_wait(x);
-                    }
-                };
-                if (edge || far) all_weights(std::true_type());
-                else all_weights(std::false_type());
                 tmem_st_wait();
                 tc_fence_before_sync();
                 __syncwarp();
@@ -267,7 +306,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
                             store_row<BF16, 32>(static_cast<__half *>(a.out) + tq * a.o_tok + hq * a.o_head + 32 * k, v);
                         } else {
 #pragma unroll
-                            for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4 *>(parts.o + pr * DIM + 32 * k + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                            for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4 *>(parts.four(2 * blockIdx.x + place, half * HALF + row_in, 32 * k + e)) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
                         }
                     }
                 }
@@ -304,22 +343,20 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
             for (int kv = 0; kv < 2; ++kv) {
                 ok = mbar_wait_warp(&code_full[kv], it & 1u, &abort_flag);
                 if (!ok) break;
-                uint4 x[LOADS];
-#pragma unroll
-                for (int k = 0; k < LOADS; ++k) {
-                    const int row = k * TOKS + tok_in;
-                    const int chunk = (DIM == 128) ? part ^ (row & 7) : part ^ ((row >> 1) & 3);
-                    x[k] = *reinterpret_cast<const uint4 *>(codes + kv * (KEYS * DIM) + row * DIM + chunk * 16);
-                }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&code_free[kv]);
                 ok = mbar_wait_warp(kv ? &v_free[st] : &k_free[st], free_parity, &abort_flag);
                 if (!ok) break;
+                const uint8_t *src = codes + kv * (KEYS * DIM);
                 uint8_t *dst = (kv ? v_smem : k_smem) + st * OPERAND + (part >> 2) * PANEL;
-#pragma unroll
-                for (int k = 0; k < LOADS; ++k) {
+                auto read = [&](int row) {
+                    const int chunk = (DIM == 128) ? part ^ (row & 7) : part ^ ((row >> 1) & 3);
+                    return *reinterpret_cast<const uint4 *>(src + row * DIM + chunk * 16);
+                };
+                uint4 x = read(tok_in);
+#pragma unroll 1
+                for (int k = 0; k < LOADS; ++k) {   // (short code: the warps of an SM's quarter all run different parts of this kernel, through one small instruction cache)
                     const int row = k * TOKS + tok_in;
-                    const uint32_t y[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+                    const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+                    if (k + 1 < LOADS) x = read(row + TOKS);
                     uint32_t z[8];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) codes_to_half<FMT>(y[e], z[2 * e], z[2 * e + 1]);
@@ -333,6 +370,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
                     *reinterpret_cast<uint4 *>(line + (((c0 + swap) ^ (row & 7)) << 4)) = swap ? v : u;
                     *reinterpret_cast<uint4 *>(line + (((c0 + 1 - swap) ^ (row & 7)) << 4)) = swap ? u : v;
                 }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&code_free[kv]);
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(kv ? &v_full[st] : &k_full[st]);
@@ -351,7 +390,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
         auto scores = [&](int half, int st) {
             const uint32_t q = q_desc + half * (OPERAND >> 4), kd = k_desc + st * (OPERAND >> 4), to = tmem + half * KEYS;
             if (issuer) {
-#pragma unroll
+#pragma unroll 2
                 for (int k = 0; k < DIM / 16; ++k) {
                     constexpr uint32_t panel = PANEL >> 4;
                     umma_f16(to, desc_of(q + (k >> 2) * panel + (k & 3) * 2, hi_desc), desc_of(kd + (k >> 2) * panel + (k & 3) * 2, hi_desc), idesc_s, k ? 1u : 0u);
@@ -364,7 +403,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
             const uint32_t vd = v_desc + st * (OPERAND >> 4), of = tmem + half * KEYS, to = tmem + 256 + half * DIM;
             const uint32_t more = first ? 0u : 1u;
             if (issuer) {
-#pragma unroll
+#pragma unroll 2
                 for (int k = 0; k < KEYS / 16; ++k) umma_f16_ts(to, of + 8 * k, desc_of(vd + k * 128, hi_desc), idesc_o, k ? 1u : more);
             }
             __syncwarp();
@@ -396,9 +435,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
             const int st = it % STAGES, sv = (it + STAGES - 1) % STAGES;
             if (halves && !begins) ok = mbar_wait_warp(&k_full[st], (it / STAGES) & 1u, &abort_flag);
             if (ok && before) ok = mbar_wait_warp(&v_full[sv], ((it - 1) / STAGES) & 1u, &abort_flag);
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                if (half >= before || !ok) break;
+#pragma unroll 1
+            for (int half = 0; half < before; ++half) {
                 ok = mbar_wait_warp(&p_full[half], p_phase[half] & 1u, &abort_flag);
                 if (!ok) break;
                 p_phase[half] += 1;
@@ -417,9 +455,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
             started = false;
             if (begins) {
                 ok = mbar_wait_warp(&k_full[st], (it / STAGES) & 1u, &abort_flag);
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    if (half >= halves || !ok) break;
+#pragma unroll 1
+                for (int half = 0; half < halves && ok; ++half) {
                     ok = mbar_wait_warp(&q_full[half], q_phase[half] & 1u, &abort_flag);
                     if (!ok) break;
                     q_phase[half] += 1;

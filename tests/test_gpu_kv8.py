@@ -263,6 +263,24 @@ def test_scales_far_apart(ctx, fmt):
     p.attend(q, [0], [0, 20])
 
 
+@pytest.mark.parametrize("fmt,d", [(0, 128), (1, 64), (1, 128)])
+@pytest.mark.parametrize("every,by", [(16, 1.7), (33, 2.5), (7, 1.3)])
+def test_maxima_that_move(ctx, fmt, d, every, by):
+    """Keys that get louder on their way: a row's largest score is passed again and again, by a little and by much, at a tile's beginning and within it; and then
+    quieter, so that nothing that comes counts."""
+    p = Pair(ctx, pages=60, heads=1, page=16, d=d, fmt=fmt, seqs=2, cols=50, seed=every)
+    first = p.reserve([0], [700])
+    k, v = p.tokens(700, "f32")
+    t = torch.arange(700, device="cuda")
+    rise = torch.where(t < 400, t, 800 - t) // every
+    k = k / k.norm(dim=2, keepdim=True) * torch.clamp(by ** rise.float(), max=3e4)[:, None, None]
+    p.store(0, k, v, [0], first, [0, 700])
+    for rows in (1, 12, 150):
+        q = torch.randn((rows, 3, d), generator=p.gen, device="cuda").half()
+        p.attend(q, [0], [0, rows])
+        p.attend(q, [0], [0, rows], causal=False, scale=0.5)
+
+
 def test_queries_of_any_size(ctx):
     """bf16 rows are brought to fp16's range by a power of two of their own; rows of zeros; a row that is not finite spoils itself alone."""
     p = Pair(ctx, pages=30, heads=1, page=16, d=128, fmt=0, seqs=2, cols=20, seed=1)
