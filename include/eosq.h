@@ -204,8 +204,9 @@ int eosq_scores(eosq_ctx *ctx, const eosq_cache_t *kcache, int64_t num_kv_heads,
  *
  * Sequences own pages through a table in device memory; whole pages may be shared by several sequences (after
  * eosq_kv8_fork), a page that is not full belongs to one.  All state is plain device memory of the caller.
- * Every call below enqueues kernels on the given stream, allocates nothing, does not synchronise and can be captured
- * into a graph.  Calls that use the same cache or the same workspace must be ordered among themselves.
+ * Every call below but eosq_kv8_check enqueues kernels on the given stream, allocates nothing, does not synchronise and can be
+ * captured into a graph (a kernel's first call loads it: make one before).  Calls that use the same cache or the same workspace must
+ * be ordered among themselves: two graphs that may run at once need a workspace each.
  *
  * Numbers in device memory (table, lengths, lists of sequences, offsets) are checked by the kernels: an entry that makes no
  * sense is skipped, nothing out of bounds is read or written, and a bit of *flags is raised (eosq_kv8_check).
@@ -279,7 +280,8 @@ int eosq_kv8_store(eosq_ctx *ctx, const eosq_kv8_t *cache, int layer, const void
  *   q, out  dev [total][kv_heads*G][d], both of dtype EOSQ_F16 or EOSQ_BF16; token and head strides in elements, d contiguous, base
  *           and strides multiples of 16 bytes; q and out do not overlap
  *   lse     dev fp32 [total][kv_heads*G], or null
- *   max_q   host, at least the largest cu[i+1] - cu[i]; an entry with more is skipped
+ *   max_q   host, at least the largest cu[i+1] - cu[i]; an entry with more is skipped.  EOSQ_ERR_UNSUPPORTED where total * G / (8, 16 or
+ *           256 rows) * kv_heads * (positions of a table row / 128) reaches 2^31
  *   workspace  eosq_kv8_workspace_bytes(cache, max_q*G)
  * Rows that belong to no entry (behind cu[n], or of a sequence of -1) are left as they are.  Sums and the statistics are held in fp32;
  * weights are rounded to fp16 before they meet the values.  `lse` lets a caller join the result with attention over other tokens

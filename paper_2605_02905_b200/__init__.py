@@ -456,10 +456,14 @@ def _kv8_rows(cache, t, heads, what):
 
 
 def _any_dtype_code(t):
-    return EOSQ_BF16 if t.dtype is _torch.bfloat16 else _dtype_code(t)
+    dtype = t.dtype
+    return EOSQ_F16 if dtype is _torch.float16 else EOSQ_BF16 if dtype is _torch.bfloat16 else _dtype_code(t)
 
 
 def _kv8_stream(cache, stream):
+    """The stream to launch on.  The memory is the current device's: a kernel of another device must not be given it."""
+    if cache._index < 0 or _torch._C._cuda_getDevice() != cache._index:
+        raise ValueError(f"the cache is on {cache.device}, which is not the current CUDA device")
     return stream.cuda_stream if stream is not None else _torch._C._cuda_getCurrentRawStream(cache._index)
 
 

@@ -387,7 +387,7 @@ struct Kv8Parts {
 template <typename T>
 __device__ __forceinline__ void kv8_cut(const Kv8Walk<T> &w, int total, int u1, int ctas) {
     Kv8Cut cut{-1, w.s.q0, w.s.m, w.r, w.h, {0, 0, 0}};
-    if (w.from == 0 && w.take > 0 && w.take < w.tiles) cut.last_cta = cta_of(total, u1 - w.reached + T::COST + w.tiles - 1, ctas);
+    if (w.from == 0 && w.take > 0 && w.take < w.tiles) cut.last_cta = min(cta_of(total, u1 - w.reached + T::COST + w.tiles - 1, ctas), ctas - 1);
     w.a.cuts[blockIdx.x] = cut;
 }
 
@@ -443,6 +443,14 @@ void launch_join(const Kv8Attend &a, int dtype, int ctas, cudaStream_t s) {
     }
 }
 
+// Whether a call with so many query rows per KV head and entry goes through the kernel for few rows (eosq_kv8_attend.cu) or the one that works on tiles of 256
+// rows (eosq_kv8_attend_tc.cu).  The first takes row tiles of 16 one after another; at d = 128 it is ahead up to 32 rows (8 x 32768 tokens 53 us, the other 62) and
+// behind from 48 on (67 against 63), at d = 64, where its codes take half the work, up to 64.
+inline bool kv8_few_rows(long long rows, int d) { return rows * d <= 4096; }
+// Row tile and key tile of the kernel that a call goes through (kv8_few_rows), for the bound on its units.
+inline int kv8_row_tile(long long rows, int d) { return kv8_few_rows(rows, d) ? (rows <= 8 ? 8 : 16) : 256; }
+constexpr int KV8_COST_BOUND = 2;   // no kernel counts a row tile's beginning and end as more units
+
 // ---- launchers ------------------------------------------------------------------------------------
 void launch_kv8_store(const Kv8 &c, int fmt, const void *const (&x)[2], int dtype, long long total, const long long (&tok)[2],
                       const long long (&head)[2], const int32_t *seqs, const int32_t *first, const int32_t *cu, int n, int max_new, cudaStream_t s);
@@ -461,10 +469,6 @@ int launch_kv8_rows(const Kv8Attend &a, int fmt, int dtype, int sm_count, cudaSt
 int launch_kv8_tiles(const Kv8Attend &a, int fmt, int dtype, int sm_count, cudaStream_t s);
 void launch_kv8_rows_join(const Kv8Attend &a, int dtype, int sm_count, cudaStream_t s);
 void launch_kv8_tiles_join(const Kv8Attend &a, int dtype, int sm_count, cudaStream_t s);
-// Whether a call with so many query rows per KV head and entry goes through the kernel for few rows (eosq_kv8_attend.cu) or the one that works on tiles of 256
-// rows (eosq_kv8_attend_tc.cu).  The first takes row tiles of 16 one after another; at d = 128 it is ahead up to 32 rows (8 x 32768 tokens 53 us, the other 62) and
-// behind from 48 on (67 against 63), at d = 64, where its codes take half the work, up to 64.
-inline bool kv8_few_rows(long long rows, int d) { return rows * d <= 4096; }
 // Tensor map over the codes of a layer's keys or values, [rows][d] bytes, in boxes of box_rows rows with a swizzle as wide as a row (eosq_tc.cu).
 bool make_code_tensor_map(const void *codes, long long rows, int d, int box_rows, CUtensorMap *out);
 

@@ -149,6 +149,10 @@ extern "C" int eosq_kv8_attend(eosq_ctx *ctx, const eosq_kv8_t *cache, int layer
             misaligned(lse, 3) || !workspace || misaligned(workspace, 255))
             return EOSQ_ERR_INVALID_ARG;
         const int most = static_cast<int>(std::min<int64_t>(max_q, total));
+        // Units (key tiles of row tiles and heads) are counted in 32 bits: there are at most total * G / row tile + n row tiles, over as many keys as a row of the table has room for.
+        const double row_tiles = static_cast<double>(total) * G / kv8_row_tile(static_cast<long long>(most) * G, cache->d) + n;
+        const double key_tiles = static_cast<double>(cache->max_pages) * cache->page_size / KV8_KEYS + 2.0 + KV8_COST_BOUND;
+        if (row_tiles * key_tiles * cache->kv_heads >= 2147483648.0) return EOSQ_ERR_UNSUPPORTED;
         if (workspace_bytes < cuts_scratch() + kv8_attend_scratch(static_cast<int64_t>(most) * G, cache->d)) return EOSQ_ERR_BUFFER_TOO_SMALL;
         if (!on_ctx_device(ctx)) return EOSQ_ERR_INVALID_ARG;
         a.seqs = seqs;

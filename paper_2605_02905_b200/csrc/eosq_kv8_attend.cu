@@ -20,7 +20,7 @@ namespace {
 // 573 instructions for 16 tokens and 286 us for 16 x 32768 tokens.
 constexpr int KEYS = KV8_KEYS, GROUP = KV8_GROUP, GROUPS = KV8_GROUPS;
 constexpr int WORKERS = 4, SHARE = KEYS / WORKERS / GROUP, THREADS = 32 * (WORKERS + 1);
-constexpr int CTAS_PER_SM = 2, COST = 2;
+constexpr int CTAS_PER_SM = 2, COST = KV8_COST_BOUND;
 
 struct TileInfo {
     int first, last;        // of the CTA's run within one row tile; first = -1: the run has ended, there is no tile

@@ -24,7 +24,7 @@ namespace {
 // instead was slower, so were scores of 64 tokens with the next 64 beside them, and twice the warps for the codes.
 constexpr int ROWS = 256, HALF = 128, KEYS = KV8_KEYS, GROUP = KV8_GROUP, GROUPS = KV8_GROUPS;
 constexpr int LOADER = 8, ISSUER = 12, FETCHER = 13, THREADS = 32 * 16, STAGES = 2, INFOS = 4;
-constexpr int COST = 2;
+constexpr int COST = KV8_COST_BOUND;
 using Tiles = Kv8Tiles<ROWS, KEYS, COST>;
 
 struct TileInfo {

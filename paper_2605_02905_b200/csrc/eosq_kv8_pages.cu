@@ -11,7 +11,8 @@ namespace {
 constexpr int PLAN_THREADS = 1024;
 constexpr int PAGES_PER_LANE = 8;   // pages that a thread looks at per step: 8192 a step, their loads under way together
 constexpr int PAGES_PER_STEP = PLAN_THREADS * PAGES_PER_LANE;
-constexpr size_t PLAN_SMEM = sizeof(int) * (2 * EOSQ_KV8_MAX_SEQS + 1);
+constexpr int FOUND = 4096;         // pages that a list may need before they are looked for a second time
+constexpr size_t PLAN_SMEM = sizeof(int) * (2 * EOSQ_KV8_MAX_SEQS + 1 + FOUND);
 
 // Exclusive prefix sum of v over the CTA, and the total.
 __device__ __forceinline__ int block_prefix(int v, int &total) {
@@ -117,7 +118,8 @@ struct ForkList {
 template <typename L, typename T, typename D>
 __device__ __forceinline__ void deal_pages(const Kv8 &c, const L &list, int n, T &&take, D &&done) {
     extern __shared__ int plan_smem[];
-    int *seen = plan_smem, *before = plan_smem + c.max_seqs;   // [max_seqs] first entry that lists a sequence; [n + 1] pages needed before an entry
+    // [max_seqs] first entry that lists a sequence; [n + 1] pages needed before an entry; [FOUND] free pages
+    int *seen = plan_smem, *before = plan_smem + c.max_seqs, *pages = before + n + 1;
     const int tid = threadIdx.x;
     unsigned flags = 0;
     for (int s = tid; s < c.max_seqs; s += PLAN_THREADS) seen[s] = INT_MAX;
@@ -128,11 +130,16 @@ __device__ __forceinline__ void deal_pages(const Kv8 &c, const L &list, int n, T
     }
     __syncthreads();
     int wanted = 0;
+    Entry mine{-1, 0, 0, -1};   // of the first PLAN_THREADS entries: this thread's
     for (int base = 0; base < n; base += PLAN_THREADS) {
         const int i = base + tid;
         // (a step adds at most 1024 * (2^20 + 1): pools have at most 2^20 pages)
         int need = 0;
-        if (i < n) need = min(max(list.get(c, i, seen, flags).need, 0), c.num_pages + 1);
+        if (i < n) {
+            const Entry e = list.get(c, i, seen, flags);
+            if (base == 0) mine = e;
+            need = min(max(e.need, 0), c.num_pages + 1);
+        }
         int total;
         const int p = block_prefix(need, total);
         if (i < n) before[i] = wanted + p;
@@ -141,8 +148,8 @@ __device__ __forceinline__ void deal_pages(const Kv8 &c, const L &list, int n, T
     if (tid == 0) before[n] = wanted;
     __syncthreads();
     auto is_free = [](int, int refs) { return refs == 0; };
-    const int have = min(each_page(c, wanted, is_free, [](int, int) {}), wanted);
-    each_page(c, have, is_free, [&](int rank, int page) {
+    const int have = min(each_page(c, wanted, is_free, [&](int rank, int page) { if (rank < FOUND) pages[rank] = page; }), wanted);
+    auto give = [&](int rank, int page) {
         if (rank >= have) return;
         int lo = 0, hi = n;   // the last entry with before[i] <= rank
         while (hi - lo > 1) {
@@ -154,14 +161,19 @@ __device__ __forceinline__ void deal_pages(const Kv8 &c, const L &list, int n, T
         unsigned unused = 0;
         take(lo, list.get(c, lo, seen, unused), rank - before[lo], page);
         c.refs[page] = 1;
-    });
+    };
+    __syncthreads();
+    if (have <= FOUND) {
+        for (int r = tid; r < have; r += PLAN_THREADS) give(r, pages[r]);
+    } else {
+        each_page(c, have, is_free, give);
+    }
     __syncthreads();
     for (int i = tid; i < n; i += PLAN_THREADS) {
-        unsigned raised = 0;
-        const Entry e = list.get(c, i, seen, raised);
+        unsigned again = 0;   // (raised before)
+        const Entry e = i < PLAN_THREADS ? mine : list.get(c, i, seen, again);
         const bool ok = e.need == 0 || (e.need > 0 && before[i] + e.need <= have);
-        if (e.need > 0 && !ok) raised |= EOSQ_KV8_NO_PAGE;
-        flags |= raised;
+        if (e.need > 0 && !ok) flags |= EOSQ_KV8_NO_PAGE;
         done(i, e, ok);
     }
     flags = __reduce_or_sync(0xffffffffu, flags);
@@ -184,6 +196,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv8_reserve_kernel(const Kv8 c, 
 // plan[i]: tokens of the new sequence (-1: refused) and the page for its last, partly filled one.
 __global__ void __launch_bounds__(PLAN_THREADS) kv8_fork_kernel(const Kv8 c, const int32_t *src, const int32_t *dst, int n, int2 *plan) {
     pdl_wait();
+    pdl_trigger();   // the copying kernel's CTAs find their places meanwhile
     deal_pages(
         c, ForkList{src, dst}, n, [&](int i, const Entry &, int, int page) { plan[i].y = page; },
         [&](int i, const Entry &e, bool ok) { plan[i].x = ok ? e.len : -1; });
@@ -286,6 +299,7 @@ __global__ void __launch_bounds__(128) kv8_free_kernel(const Kv8 c, const int32_
 constexpr int MOVES_AT = 64;
 __global__ void __launch_bounds__(PLAN_THREADS) kv8_compact_kernel(const Kv8 c, int32_t *remap, int32_t *moves) {
     pdl_wait();
+    pdl_trigger();
     const int used = each_page(c, INT_MAX, [](int, int refs) { return refs != 0; }, [](int, int) {});
     int32_t *list = moves + MOVES_AT;
     const int both = each_page(
@@ -328,12 +342,12 @@ __global__ void __launch_bounds__(COPY_THREADS) kv8_move_kernel(const Kv8 c, con
 
 bool launch_kv8_reserve(const Kv8 &c, const int32_t *seqs, const int32_t *add, int n, int32_t *first, cudaStream_t s) {
     if (!ensure_dynamic_smem(reinterpret_cast<const void *>(kv8_reserve_kernel), PLAN_SMEM)) return false;
-    launch_dependent(kv8_reserve_kernel, dim3(1), PLAN_THREADS, sizeof(int) * (c.max_seqs + n + 1), s, c, seqs, add, n, first);
+    launch_dependent(kv8_reserve_kernel, dim3(1), PLAN_THREADS, sizeof(int) * (c.max_seqs + n + 1 + FOUND), s, c, seqs, add, n, first);
     return true;
 }
 bool launch_kv8_fork(const Kv8 &c, const int32_t *src, const int32_t *dst, int n, int2 *plan, cudaStream_t s) {
     if (!ensure_dynamic_smem(reinterpret_cast<const void *>(kv8_fork_kernel), PLAN_SMEM)) return false;
-    launch_dependent(kv8_fork_kernel, dim3(1), PLAN_THREADS, sizeof(int) * (c.max_seqs + n + 1), s, c, src, dst, n, plan);
+    launch_dependent(kv8_fork_kernel, dim3(1), PLAN_THREADS, sizeof(int) * (c.max_seqs + n + 1 + FOUND), s, c, src, dst, n, plan);
     return true;
 }
 void launch_kv8_fork_copy(const Kv8 &c, const int32_t *src, const int32_t *dst, int n, const int2 *plan, cudaStream_t s) {

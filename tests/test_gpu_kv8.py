@@ -218,6 +218,7 @@ def test_attention_of_a_token(ctx, fmt, dtype, d, page, heads, G):
     p.attend(q, seqs, list(range(n + 1)), window=1)
     p.attend(q, seqs, list(range(n + 1)), window=70)
     p.attend(q * 30, seqs, list(range(n + 1)), scale=-0.2)   # weights far apart
+    p.attend(q, seqs, list(range(n + 1)), scale=0.0)         # all alike
 
 
 @pytest.mark.parametrize("fmt", [0, 1])
@@ -236,6 +237,8 @@ def test_attention_of_many_queries(ctx, fmt, dtype, d, page, heads, G, news):
     p.attend(q, seqs, cu, causal=False)
     p.attend(q, seqs, cu, window=9, most=cu[-1] + 3)
     p.attend(q, seqs, cu, window=150)
+    p.attend(q, seqs, cu, scale=-0.3)
+    p.attend(q, seqs, cu, scale=0.0, window=77)
 
 
 @pytest.mark.parametrize("rows", [1, 40])

@@ -80,7 +80,7 @@ def test_no_context(name):
     ("store", dict(total=0), OK), ("store", dict(most=0), OK), ("store", dict(dtype=1, stride=1026), INVALID), ("attend", dict(total=0), OK), ("attend", dict(most=0), OK),
     ("attend", dict(dtype=1), INVALID), ("attend", dict(G=0), INVALID), ("attend", dict(window=-1), INVALID), ("attend", dict(window=5, causal=0), INVALID),
     ("attend", dict(scale=float("nan")), INVALID), ("attend", dict(scale=float("inf")), INVALID), ("attend", dict(lse=P + 2), INVALID),
-    ("store", dict(total=1 << 31), UNSUPPORTED), ("attend", dict(total=1 << 31), UNSUPPORTED), ("copy_pages", dict(n=(1 << 20) + 1), UNSUPPORTED),
+    ("attend", dict(total=(1 << 31) - 1, most=1, G=64), UNSUPPORTED), ("store", dict(total=1 << 31), UNSUPPORTED), ("attend", dict(total=1 << 31), UNSUPPORTED), ("copy_pages", dict(n=(1 << 20) + 1), UNSUPPORTED),
 ])
 def test_arguments_that_are_refused(name, bad, want):
     assert _calls(_cache(), **bad)[name]() == want
@@ -120,6 +120,10 @@ def test_the_handle():
     for args in ((q[:, :, :32], i[:1], i), (q[:, :5], i[:1], i), (q, i[:1].long(), i), (q, i[:1], i[:1])):
         with pytest.raises(ValueError):
             eosq.eosq_kv8_attend(NoContext, c, 0, *args, 2)
+    for call in (lambda: eosq.eosq_kv8_free(NoContext, c, i), lambda: eosq.eosq_kv8_check(NoContext, c), lambda: eosq.eosq_kv8_compact(NoContext, c),
+                 lambda: eosq.eosq_kv8_attend(NoContext, c, 0, q, i[:1], i, 2)):
+        with pytest.raises(ValueError, match="not the current CUDA device"):
+            call()
     with pytest.raises(TypeError):
         eosq.eosq_kv8_store(NoContext, c, 0, q.double()[:, :3], q.double()[:, :3], i[:1], i[:1], i, 2)
 
