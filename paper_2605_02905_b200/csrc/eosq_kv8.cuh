@@ -443,12 +443,12 @@ void launch_join(const Kv8Attend &a, int dtype, int ctas, cudaStream_t s) {
     }
 }
 
-// Whether a call with so many query rows per KV head and entry goes through the kernel for few rows (eosq_kv8_attend.cu) or the one that works on tiles of 256
-// rows (eosq_kv8_attend_tc.cu).  The first takes row tiles of 16 one after another; at d = 128 it is ahead up to 32 rows (8 x 32768 tokens 53 us, the other 62) and
-// behind from 48 on (67 against 63), at d = 64, where its codes take half the work, up to 64.
-inline bool kv8_few_rows(long long rows, int d) { return rows * d <= 4096; }
-// Row tile and key tile of the kernel that a call goes through (kv8_few_rows), for the bound on its units.
-inline int kv8_row_tile(long long rows, int d) { return kv8_few_rows(rows, d) ? (rows <= 8 ? 8 : 16) : 256; }
+// Which kernel a call goes through: the one for few rows (eosq_kv8_attend.cu), which takes row tiles of 16 one after another, or the one that works on tiles of 256 rows
+// (eosq_kv8_attend_tc.cu).  most: rows (queries times heads of a group) of the longest entry, rows: of all n entries, per KV head.  With equal entries the first
+// is ahead up to 32 rows at d = 128 (8 heads, 32768 tokens: 54 us, the other 61; 48 rows: 65 and 61) and up to 48 at d = 64, where its codes take half the work
+// (43 and 47; 64 rows: 49 and 47); what counts is the mean, since its time goes by row tiles of 16 and the other's by entries (24 of 1 to 60 rows, d = 64: 25
+// and 38).
+inline bool kv8_few_rows(long long most, long long rows, int n, int d) { return most <= 16 || rows <= static_cast<long long>(n) * (d == 128 ? 40 : 56); }
 constexpr int KV8_COST_BOUND = 2;   // no kernel counts a row tile's beginning and end as more units
 
 // ---- launchers ------------------------------------------------------------------------------------

@@ -73,7 +73,7 @@ int entry(F &&f) {
 size_t pages_scratch(const eosq_kv8_t *c) {
     return std::max(sizeof(int2) * static_cast<size_t>(c->max_seqs), sizeof(int32_t) * (64 + static_cast<size_t>(c->num_pages)));
 }
-size_t kv8_attend_scratch(int64_t rows, int d) { return kv8_few_rows(rows, d) ? kv8_rows_scratch(d) : kv8_tiles_scratch(d); }
+size_t kv8_attend_scratch(int64_t most, int d) { return most <= 16 ? kv8_rows_scratch(d) : std::max(kv8_rows_scratch(d), kv8_tiles_scratch(d)); }
 size_t cuts_scratch() { return align_up(sizeof(Kv8Cut) * KV8_MAX_CTAS, 256); }
 
 int set_up_failed(eosq_ctx *ctx, const char *what) {
@@ -150,7 +150,9 @@ extern "C" int eosq_kv8_attend(eosq_ctx *ctx, const eosq_kv8_t *cache, int layer
             return EOSQ_ERR_INVALID_ARG;
         const int most = static_cast<int>(std::min<int64_t>(max_q, total));
         // Units (key tiles of row tiles and heads) are counted in 32 bits: there are at most total * G / row tile + n row tiles, over as many keys as a row of the table has room for.
-        const double row_tiles = static_cast<double>(total) * G / kv8_row_tile(static_cast<long long>(most) * G, cache->d) + n;
+        const int64_t most_rows = static_cast<int64_t>(most) * G;
+        const bool few = kv8_few_rows(most_rows, total * G, n, cache->d);
+        const double row_tiles = static_cast<double>(total) * G / (few ? (most_rows <= 8 ? 8 : 16) : 256) + n;
         const double key_tiles = static_cast<double>(cache->max_pages) * cache->page_size / KV8_KEYS + 2.0 + KV8_COST_BOUND;
         if (row_tiles * key_tiles * cache->kv_heads >= 2147483648.0) return EOSQ_ERR_UNSUPPORTED;
         if (workspace_bytes < cuts_scratch() + kv8_attend_scratch(static_cast<int64_t>(most) * G, cache->d)) return EOSQ_ERR_BUFFER_TOO_SMALL;
@@ -177,7 +179,6 @@ extern "C" int eosq_kv8_attend(eosq_ctx *ctx, const eosq_kv8_t *cache, int layer
         a.err = ctx->dev_err;
         cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
         int why = 0;
-        const bool few = kv8_few_rows(static_cast<long long>(most) * G, cache->d);
         run_stage(ctx, ST_OTHER, s, [&] {
             why = few ? launch_kv8_rows(a, cache->format, dtype, ctx->sm_count, s) : launch_kv8_tiles(a, cache->format, dtype, ctx->sm_count, s);
         });
