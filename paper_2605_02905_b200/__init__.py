@@ -450,7 +450,7 @@ def _kv8_list(cache, t, n, what):
 def _kv8_rows(cache, t, heads, what):
     """Data pointer and strides of [total][heads][d], d contiguous."""
     stride = t.stride()
-    if len(stride) != 3 or t.shape[1:] != (heads, cache.d) or t.get_device() != cache._index or stride[2] != 1:
+    if len(stride) != 3 or stride[2] != 1 or t.size(1) != heads or t.size(2) != cache.d or t.get_device() != cache._index:
         raise ValueError(f"{what}: [total][{heads}][{cache.d}] with contiguous rows on {cache.device} is wanted, not {list(t.shape)} on {t.device}")
     return t.data_ptr(), stride[0], stride[1]
 
@@ -520,17 +520,19 @@ def eosq_kv8_store(ctx: Context, cache: Kv8Cache, layer: int, k, v, seqs, first,
 def eosq_kv8_attend(ctx: Context, cache: Kv8Cache, layer: int, q, seqs, cu, max_q: int, scale: Optional[float] = None, causal: bool = True,
                     window: int = 0, out=None, lse=None, want_lse: bool = False, workspace=None, stream=None):
     """q: [total][kv_heads * G][d] fp16 or bf16.  Returns out, or (out, lse) with want_lse (or with an lse to write to)."""
+    if q.dim() != 3:
+        raise ValueError(f"q: [total][heads][{cache.d}] is wanted, not {list(q.shape)}")
     n = seqs.size(0)
-    total, H = q.shape[0], q.shape[1]
-    if H % cache.kv_heads or H == 0:
-        raise ValueError(f"q has {H} heads, not a multiple of {cache.kv_heads}")
+    total, H, _ = q.size()
     G = H // cache.kv_heads
+    if H == 0 or G * cache.kv_heads != H:
+        raise ValueError(f"q has {H} heads, not a multiple of {cache.kv_heads}")
     qp, qt, qh = _kv8_rows(cache, q, H, "q")
     if out is None:
         out = _torch.empty_like(q) if stream is None and q.is_contiguous() else _new(q, (total, H, cache.d), q.dtype, stream)
         op, ot, oh = out.data_ptr(), H * cache.d, cache.d
     else:
-        if out.dtype is not q.dtype or out.shape[0] != total:
+        if out.dtype is not q.dtype or out.size(0) != total:
             raise ValueError(f"out: {q.dtype} [{total}][{H}][{cache.d}] is wanted")
         op, ot, oh = _kv8_rows(cache, out, H, "out")
     if want_lse and lse is None:

@@ -104,6 +104,7 @@ struct Kv8Attend {
     Kv8 c;
     const int32_t *seqs, *cu;
     int n, max_q, G, causal, window;
+    int whole;                                 // row tiles are not shared between CTAs: a unit is one of them with a head
     long long total;
     const void *q;
     void *out;
@@ -128,6 +129,8 @@ struct Kv8Tiles {
         lo = a.window > 0 ? max(s.len - s.m + t0 - a.window + 1, 0) : 0;
     }
     static __device__ __forceinline__ int row_tiles(const Kv8Attend &a, const Kv8Seq &s) { return (s.m * a.G + RT - 1) / RT; }
+    // Units of a row tile of so many key tiles and a head.
+    static __device__ __forceinline__ int units(const Kv8Attend &a, int tiles) { return a.whole ? 1 : tiles + COST; }
     // First key tile of row tile r, and how many: at least one, so that rows which see nothing are written too.
     static __device__ __forceinline__ int key_tiles(const Kv8Attend &a, const Kv8Seq &s, int r, int &first) {
         int lo, hi;
@@ -177,18 +180,18 @@ struct Kv8Walk {
                         continue;
                     }
                     tiles = T::key_tiles(a, s, r, tile0);
-                    const int all = (tiles + T::COST) * a.c.heads;
+                    const int all = T::units(a, tiles) * a.c.heads;
                     if (at < all) break;
                     at -= all;
                     ++r;
                 }
-                h = at / (tiles + T::COST);
-                at -= h * (tiles + T::COST);
+                h = at / T::units(a, tiles);
+                at -= h * T::units(a, tiles);
             }
-            reached = at + min(tiles + T::COST - at, left);
+            reached = at + min(T::units(a, tiles) - at, left);
             left -= reached - at;
-            from = max(at - T::COST, 0);
-            take = max(reached - T::COST, 0) - from;
+            from = a.whole ? 0 : max(at - T::COST, 0);
+            take = a.whole ? tiles : max(reached - T::COST, 0) - from;
             at = 0;
             if (take > 0) return true;
         }
@@ -332,7 +335,7 @@ __device__ __forceinline__ Kv8Run kv8_run(const Kv8Attend &a, int *units) {
         if (s.m > 0) {
             const int tiles = T::row_tiles(a, s);
             int first;
-            for (int r = 0; r < tiles; ++r) u += T::key_tiles(a, s, r, first) + T::COST;
+            for (int r = 0; r < tiles; ++r) u += T::units(a, T::key_tiles(a, s, r, first));
         }
         units[i] = u * a.c.heads;
     }

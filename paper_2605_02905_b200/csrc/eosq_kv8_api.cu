@@ -164,6 +164,11 @@ extern "C" int eosq_kv8_attend(eosq_ctx *ctx, const eosq_kv8_t *cache, int layer
         a.G = G;
         a.causal = causal != 0;
         a.window = window;
+        // Rows of the table that hold few tokens: what CTAs could share of a row tile is less than joining it would cost, and the second kernel is not needed.
+        // Shared and joined / whole, one query a sequence, 8 heads: 10.6 / 9.0 us at one sequence of 300 tokens, 15.3 / 11.8 at 19 of 440, 20.2 / 17.2 at 64
+        // of 300, 16.7 / 16.8 at 64 of 1 to 500; 22.1 / 23.9 at 100 queries on 300 tokens and 25.6 / 22.4 at 300 queries.  With many row tiles to a CTA
+        // what is saved falls (52.6 / 48.2 at 256) and runs of long sequences would make some CTAs late.
+        a.whole = static_cast<int64_t>(cache->max_pages) * cache->page_size <= 4 * KV8_KEYS && row_tiles * cache->kv_heads <= 8.0 * ctx->sm_count;
         a.total = total;
         a.q = q;
         a.out = out;
@@ -183,7 +188,7 @@ extern "C" int eosq_kv8_attend(eosq_ctx *ctx, const eosq_kv8_t *cache, int layer
             why = few ? launch_kv8_rows(a, cache->format, dtype, ctx->sm_count, s) : launch_kv8_tiles(a, cache->format, dtype, ctx->sm_count, s);
         });
         if (why) return set_up_failed(ctx, "eosq_kv8_attend: tensor map or launch set-up failed");
-        run_stage(ctx, ST_OTHER, s, [&] {
+        if (!a.whole) run_stage(ctx, ST_OTHER, s, [&] {
             if (few) launch_kv8_rows_join(a, dtype, ctx->sm_count, s);
             else launch_kv8_tiles_join(a, dtype, ctx->sm_count, s);
         });

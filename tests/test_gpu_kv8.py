@@ -241,6 +241,19 @@ def test_attention_of_many_queries(ctx, fmt, dtype, d, page, heads, G, news):
     p.attend(q, seqs, cu, scale=0.0, window=77)
 
 
+@pytest.mark.parametrize("cols,page", [(4, 128), (5, 128), (32, 16)])
+@pytest.mark.parametrize("rows,G", [(1, 2), (3, 9), (140, 2)])
+def test_attention_where_a_row_of_the_table_is_short(ctx, cols, page, rows, G):
+    """Up to 512 tokens to a sequence row tiles are not shared between CTAs; above that they may be."""
+    p = Pair(ctx, pages=200, heads=3, page=page, d=64, seqs=5, cols=cols, seed=2)
+    p.append([0, 1, 2, 3], [512, 511, 1, 300])
+    q = torch.randn((4 * rows, 3 * G, 64), generator=p.gen, device="cuda").half()
+    cu = [rows * i for i in range(5)]
+    p.attend(q, [3, 0, 1, 2], cu)
+    p.attend(q, [3, 0, 1, 2], cu, window=100)
+    p.attend(q, [3, 0, 4, 2], cu, causal=False)
+
+
 @pytest.mark.parametrize("rows", [1, 40])
 def test_attention_over_a_long_cache(ctx, rows):
     """Many CTAs share a row tile; the whole call is one sequence's, or one long one's among short ones."""
