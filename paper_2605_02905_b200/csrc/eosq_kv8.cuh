@@ -395,7 +395,7 @@ __device__ __forceinline__ void kv8_cut(const Kv8Walk<T> &w, int total, int u1, 
 }
 
 // Row tiles that several CTAs worked on: their partial results under one maximum, in the order of the keys.  A CTA of this kernel per 16 rows (or 8) and
-// CTA of the other, which a row tile may begin in and not end.
+// CTA of the other, which a row tile may begin in and not end.  It is a launch behind the last CTA's end and a chain of three loads: some 3 us.
 template <int RT, int DIM, bool BF16>
 __global__ void __launch_bounds__(128) kv8_join_kernel(const Kv8Attend a, int ctas) {
     pdl_wait();
