@@ -20,12 +20,12 @@ namespace {
 // 573 instructions for 16 tokens and 286 us for 16 x 32768 tokens.
 // What bounds it is the memory: those tokens, 8 heads of 128 with four queries each, take 170 us, 6.3 TB/s of codes (a copy reaches 6.46), with half the issue
 // slots in use.  Short of that it is the way to the first tile: 1.4 us (48 entries: 2.4) until a CTA knows its run, 1.3 for a page's number, as much for its scales, 2
-// for the codes, 2 for the queries, which wait behind other CTAs' codes; then 1 us a tile until the code has been fetched.  48 x 64 .. 8192 tokens: 43 us, 26.5 at a copy's rate.
+// for the codes, 2 for the queries, which wait behind other CTAs' codes; then 1 us a tile until the code has been fetched.  48 x 64 .. 8192 tokens: 40 us, 26.5 at a copy's rate.
 // Queries brought by the fetching warp with the codes gained 2 % there and lost 3 % at d = 64 and on one short sequence; codes asked for before
 // their scales are known gained nothing.
 constexpr int KEYS = KV8_KEYS, GROUP = KV8_GROUP, GROUPS = KV8_GROUPS;
 constexpr int WORKERS = 4, SHARE = KEYS / WORKERS / GROUP, THREADS = 32 * (WORKERS + 1);
-constexpr int CTAS_PER_SM = 2, COST = KV8_COST_BOUND;
+constexpr int CTAS_PER_SM = 2, COST = 2;   // (one unit or three for a row tile: 43.5 and 41.4 us for those 48 sequences, 39.8 so)
 
 struct TileInfo {
     int first, last;        // of the CTA's run within one row tile; first = -1: the run has ended, there is no tile
@@ -126,8 +126,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
         if (now.tiles) fetch.scales(now);
         Kv8Batch next = fetch.next();
         while (ok && now.tiles) {
-            if (next.tiles) fetch.scales(next);
-            const Kv8Batch after = next.tiles ? fetch.next() : next;
+            Kv8Batch after = next;
             const float ks = now.ks * a.scale_log2;
             const float vs = fminf(fmaxf(now.vs, KV8_SCALE_MIN), KV8_SCALE_MAX);
             const float vlog = now.page >= 0 ? log2f(vs) : -INFINITY, vinv = 1.0f / vs;
@@ -167,6 +166,10 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
                     tma_load_2d(dst + TILE, &vmap, &full_bar[st], 0, row);
                 }
                 __syncwarp();
+                if (t == 0 && next.tiles) {   // (behind this batch's first copies, which need not wait for the next one's pages)
+                    fetch.scales(next);
+                    after = fetch.next();
+                }
             }
             now = next;
             next = after;

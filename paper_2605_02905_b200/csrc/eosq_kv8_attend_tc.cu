@@ -21,12 +21,15 @@ namespace {
 //   warps 14, 15     bring the next row tile's queries in as soon as this one's last scores have been made
 // A half's chain is what bounds it: products of 128 x 128 x d twice (some 1500 cycles, shared memory feeding them), then the weights of a row per thread (some 2500, of
 // which the special function units need 1024, or 2048 where the halves meet); the halves overlap, so a tile takes some 4800 cycles: four prompts
-// of 2048 queries on 12000 tokens run at 1012 TFLOP/s (1717 for a library product), four of 500 to 2048 on 2048 to 12000, with their diagonal and their
-// last row tiles, at 800.  Half the weights' 2^x by a polynomial
+// of 2048 queries on 12000 tokens run at 1014 TFLOP/s (1717 for a library product), four of 500 to 2048 on 2048 to 12000, with their diagonal and their
+// last row tiles, at 905.  Half the weights' 2^x by a polynomial
 // instead was slower, so were scores of 64 tokens with the next 64 beside them, and twice the warps for the codes.
 constexpr int ROWS = 256, HALF = 128, KEYS = KV8_KEYS, GROUP = KV8_GROUP, GROUPS = KV8_GROUPS;
 constexpr int LOADER = 8, ISSUER = 12, FETCHER = 13, THREADS = 32 * 16, STAGES = 2, INFOS = 4;
-constexpr int COST = KV8_COST_BOUND;
+// A row tile's beginning and end (queries in, a first tile looked at twice, results out, nothing of one half beside the other's) take as long as five tiles with bf16
+// queries, as three and a half with fp16: four prompts of 500 to 2048 queries, bf16 / fp16, 623 / 499 us counted as two, 550 / 465 as four, 544 / 463 as five, 539 / 465 as six.
+constexpr int COST = 5;
+static_assert(COST <= KV8_COST_BOUND, "the bound on a call's units");
 using Tiles = Kv8Tiles<ROWS, KEYS, COST>;
 
 struct TileInfo {
@@ -85,7 +88,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
         }
         for (int i = 0; i < INFOS; ++i) {
             mbar_init(&info_full[i], 1);
-            mbar_init(&info_free[i], 15);   // all warps but the one that fills them
+            mbar_init(&info_free[i], ISSUER + 1);   // the warps that read them
         }
         mbar_init(&drain_bar, 1);
         abort_flag = 0;
@@ -480,30 +483,32 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
         constexpr int LANES = DIM / 8, PER = 32 / LANES, LOADS = HALF / 2 / PER;   // lanes of a row, rows of an instruction, instructions
         const int part = lane % LANES, row_lane = (warp - FETCHER - 1) * (HALF / 2) + lane / LANES;
         const uint32_t flip = (a.scale_log2 < 0.0f) ? 0x80008000u : 0u;
+        const int step_t = PER / a.G, step_g = PER - step_t * a.G;
         uint32_t uses[2] = {0, 0}, items = 0;
         bool ok = true;
-        for (uint32_t it = 0; ok; ++it) {
-            const int slot = it % INFOS;
-            ok = mbar_wait_warp(&info_full[slot], (it / INFOS) & 1u, &abort_flag);
-            if (!ok) break;
-            const TileInfo &ti = info[slot];
-            const int end = ti.end, first = ti.first, q0 = ti.q0, rows = ti.m * a.G, r = ti.r, h = ti.h;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&info_free[slot]);
-            if (end < 0) break;
-            if (!first) continue;
+        Kv8Walk<Tiles> w(a, run.entry, run.skip, run.u1 - run.u0);   // (of their own: the first queries come beside the first pages, scales and codes)
+        while (ok && w.next()) {
+            const int rows = w.s.m * a.G;
             for (int half = 0; half < 2 && ok; ++half) {
-                const int row0 = r * ROWS + half * HALF;
+                const int row0 = w.r * ROWS + half * HALF;
                 if (row0 >= rows) break;
                 ok = mbar_wait_warp(&q_free[half], (uses[half] & 1u) ^ 1u, &abort_flag);
                 if (!ok) break;
                 uses[half] += 1;
                 auto place = [&](int at) { return q_smem + half * OPERAND + (part >> 3) * PANEL + at * 128 + (((part & 7) ^ (at & 7)) << 4); };
+                int t = (row0 + row_lane) / a.G, g = row0 + row_lane - t * a.G;
 #pragma unroll 4
                 for (int k = 0; k < LOADS; ++k) {
-                    const int at = row_lane + k * PER, row = row0 + at, t = min(row, rows - 1) / a.G;
-                    const __half *src = static_cast<const __half *>(a.q) + (q0 + static_cast<long long>(t)) * a.q_tok + (h * a.G + min(row, rows - 1) - t * a.G) * a.q_head + part * 8;
-                    cp_async16(place(at), src, row < rows);
+                    const int at = row_lane + k * PER;
+                    const bool there = row0 + at < rows;
+                    const long long from = there ? (w.s.q0 + static_cast<long long>(t)) * a.q_tok + (w.h * a.G + g) * a.q_head + part * 8 : 0;
+                    cp_async16(place(at), static_cast<const __half *>(a.q) + from, there);
+                    t += step_t;
+                    g += step_g;
+                    if (g >= a.G) {
+                        g -= a.G;
+                        t += 1;
+                    }
                 }
                 cp_async_wait_all();
                 __syncwarp();
@@ -561,8 +566,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
         if (now.tiles) fetch.scales(now);
         Kv8Batch next = fetch.next();
         while (ok && now.tiles) {
-            if (next.tiles) fetch.scales(next);
-            const Kv8Batch after = next.tiles ? fetch.next() : next;
+            Kv8Batch after = next;
             const float vs = fminf(fmaxf(now.vs, KV8_SCALE_MIN), KV8_SCALE_MAX);
             const float vlog = now.page >= 0 ? log2f(vs) : -INFINITY, vinv = 1.0f / vs;
             int row;
@@ -607,6 +611,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
                     __syncwarp();
                 }
                 if (!ok) break;
+                if (t == 0 && next.tiles) {   // (behind this batch's first copies, which need not wait for the next one's pages)
+                    fetch.scales(next);
+                    after = fetch.next();
+                }
             }
             now = next;
             next = after;
