@@ -104,6 +104,7 @@ struct Kv8Attend {
     Kv8 c;
     const int32_t *seqs, *cu;
     int n, max_q, G, causal, window;
+    int rows_min, rows_max;                    // entries of fewer or more rows than this are another launch's
     int whole;                                 // row tiles are not shared between CTAs: a unit is one of them with a head
     long long total;
     const void *q;
@@ -115,6 +116,13 @@ struct Kv8Attend {
     float *part;                               // scratch: partial results, two slots per CTA
     int *err;
 };
+
+// Entry i of a call, with m = 0 where it is another launch's.
+__device__ __forceinline__ Kv8Seq kv8_seq(const Kv8Attend &a, int i) {
+    Kv8Seq s = kv8_seq(a.c, a.seqs, a.cu, i, a.total, a.max_q);
+    if (s.m * a.G < a.rows_min || s.m * a.G > a.rows_max) s.m = 0;
+    return s;
+}
 
 // The work of one call: every entry's query rows (query t, head g of a KV head: row t * G + g) cut into tiles of RT, the keys that
 // a row tile sees cut into tiles of KT.  A unit is one key tile of one row tile and KV head, or one of COST that stand for a row tile's beginning and
@@ -160,7 +168,7 @@ struct Kv8Walk {
         if (left > 0) enter();
     }
     __device__ __forceinline__ void enter() {
-        s = kv8_seq(a.c, a.seqs, a.cu, i, a.total, a.max_q);
+        s = kv8_seq(a, i);
         row_tiles = (s.m > 0) ? T::row_tiles(a, s) : 0;
         r = 0;
     }
@@ -330,7 +338,7 @@ __device__ __forceinline__ Kv8Run kv8_run(const Kv8Attend &a, int *units) {
     __shared__ int total_units;
     const int tid = threadIdx.x;
     for (int i = tid; i < a.n; i += THREADS) {
-        const Kv8Seq s = kv8_seq(a.c, a.seqs, a.cu, i, a.total, a.max_q);
+        const Kv8Seq s = kv8_seq(a, i);
         int u = 0;
         if (s.m > 0) {
             const int tiles = T::row_tiles(a, s);
@@ -468,10 +476,17 @@ void launch_join(const Kv8Attend &a, int dtype, int ctas, cudaStream_t s) {
 
 // Which kernel a call goes through: the one for few rows (eosq_kv8_attend.cu), which takes row tiles of 16 one after another, or the one that works on tiles of 256 rows
 // (eosq_kv8_attend_tc.cu).  most: rows (queries times heads of a group) of the longest entry, rows: of all n entries, per KV head.  With equal entries the first
-// is ahead up to 32 rows at d = 128 (8 heads, 32768 tokens: 54 us, the other 61; 48 rows: 65 and 61) and up to 48 at d = 64, where its codes take half the work
-// (43 and 47; 64 rows: 49 and 47); what counts is the mean, since its time goes by row tiles of 16 and the other's by entries (24 of 1 to 60 rows, d = 64: 25
-// and 38).
-inline bool kv8_few_rows(long long most, long long rows, int n, int d) { return most <= 16 || rows <= static_cast<long long>(n) * (d == 128 ? 40 : 56); }
+// is ahead up to 32 rows at d = 128 (8 heads, 32768 tokens: 41 us, the other 50; 48 rows: 56 and 50) and up to 48 at d = 64, where its codes take half the work
+// (38 and 42; 64 rows: 46 and 42); what counts is the mean, since its time goes by row tiles of 16 and the other's by entries (24 of 1 to 60 rows, d = 64: 23
+// and 36).
+inline bool kv8_few_rows(long long most, long long rows, int n, int d) { return most <= 16 || rows <= static_cast<long long>(n) * (d == 128 ? 36 : 52); }
+// Both, where a prompt's chunk comes with sequences that get a token each: entries of up to so many rows through the first and then the others through the second; 0: one
+// of them takes all.  8 heads, G = 4, d = 128, through one kernel / both: 63 single tokens on 4096 each and a chunk of 512 queries 347 / 168 us, with a chunk of 128
+// 179 / 139; 31 on 2000 and a chunk of 512 on 16000 231 / 201; 63 on 500 with one of 128 44 / 48, two more launches; 7 on 1000 with one of 128 51 / 54.
+inline int kv8_split(long long most, long long rows, int n, int G) {
+    if (most < 512 || rows > n * (most / 4) || G > 16) return 0;
+    return G <= 8 ? 8 : 16;
+}
 constexpr int KV8_COST_BOUND = 5;   // no kernel counts a row tile's beginning and end as more units
 
 // ---- launchers ------------------------------------------------------------------------------------

@@ -151,7 +151,8 @@ extern "C" int eosq_kv8_attend(eosq_ctx *ctx, const eosq_kv8_t *cache, int layer
         const int most = static_cast<int>(std::min<int64_t>(max_q, total));
         // Units (key tiles of row tiles and heads) are counted in 32 bits: there are at most total * G / row tile + n row tiles, over as many keys as a row of the table has room for.
         const int64_t most_rows = static_cast<int64_t>(most) * G;
-        const bool few = kv8_few_rows(most_rows, total * G, n, cache->d);
+        const int split = kv8_split(most_rows, total * G, n, G);
+        const bool few = !split && kv8_few_rows(most_rows, total * G, n, cache->d);
         const double row_tiles = static_cast<double>(total) * G / (few ? (most_rows <= 8 ? 8 : 16) : 256) + n;
         const double key_tiles = static_cast<double>(cache->max_pages) * cache->page_size / KV8_KEYS + 2.0 + KV8_COST_BOUND;
         if (row_tiles * key_tiles * cache->kv_heads >= 2147483648.0) return EOSQ_ERR_UNSUPPORTED;
@@ -183,15 +184,20 @@ extern "C" int eosq_kv8_attend(eosq_ctx *ctx, const eosq_kv8_t *cache, int layer
         a.part = reinterpret_cast<float *>(p + cuts_scratch());
         a.err = ctx->dev_err;
         cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-        int why = 0;
-        run_stage(ctx, ST_OTHER, s, [&] {
-            why = few ? launch_kv8_rows(a, cache->format, dtype, ctx->sm_count, s) : launch_kv8_tiles(a, cache->format, dtype, ctx->sm_count, s);
-        });
-        if (why) return set_up_failed(ctx, "eosq_kv8_attend: tensor map or launch set-up failed");
-        if (!a.whole) run_stage(ctx, ST_OTHER, s, [&] {
-            if (few) launch_kv8_rows_join(a, dtype, ctx->sm_count, s);
-            else launch_kv8_tiles_join(a, dtype, ctx->sm_count, s);
-        });
+        for (const bool rows : {true, false}) {
+            if (!split && rows != few) continue;
+            a.rows_min = (split && !rows) ? split + 1 : 1;
+            a.rows_max = (split && rows) ? split : static_cast<int>(most_rows);
+            int why = 0;
+            run_stage(ctx, ST_OTHER, s, [&] {
+                why = rows ? launch_kv8_rows(a, cache->format, dtype, ctx->sm_count, s) : launch_kv8_tiles(a, cache->format, dtype, ctx->sm_count, s);
+            });
+            if (why) return set_up_failed(ctx, "eosq_kv8_attend: tensor map or launch set-up failed");
+            if (!a.whole) run_stage(ctx, ST_OTHER, s, [&] {
+                if (rows) launch_kv8_rows_join(a, dtype, ctx->sm_count, s);
+                else launch_kv8_tiles_join(a, dtype, ctx->sm_count, s);
+            });
+        }
         return record_cuda(ctx, cudaGetLastError(), "eosq_kv8_attend launch") ? EOSQ_ERR_CUDA : EOSQ_OK;
     });
 }

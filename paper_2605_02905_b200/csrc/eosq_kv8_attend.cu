@@ -530,7 +530,7 @@ bool launch_rows(const Kv8Attend &a, bool i8, bool bf, int sm_count, cudaStream_
 size_t kv8_rows_scratch(int d) { return sizeof(float) * 2 * KV8_MAX_CTAS * 16 * (static_cast<size_t>(d) + 2); }
 
 int launch_kv8_rows(const Kv8Attend &a, int fmt, int dtype, int sm_count, cudaStream_t s) {
-    const bool bf = dtype == EOSQ_BF16, i8 = fmt == EOSQ_KV_INT8, eight = a.max_q * a.G <= 8;
+    const bool bf = dtype == EOSQ_BF16, i8 = fmt == EOSQ_KV_INT8, eight = a.rows_max <= 8;
     bool ok;
     if (a.c.d_shift == 7) ok = eight ? launch_rows<128, 1>(a, i8, bf, sm_count, s) : launch_rows<128, 2>(a, i8, bf, sm_count, s);
     else ok = eight ? launch_rows<64, 1>(a, i8, bf, sm_count, s) : launch_rows<64, 2>(a, i8, bf, sm_count, s);
@@ -538,7 +538,7 @@ int launch_kv8_rows(const Kv8Attend &a, int fmt, int dtype, int sm_count, cudaSt
 }
 
 void launch_kv8_rows_join(const Kv8Attend &a, int dtype, int sm_count, cudaStream_t s) {
-    if (a.max_q * a.G <= 8) launch_join<8>(a, dtype, ctas_of(sm_count), s);
+    if (a.rows_max <= 8) launch_join<8>(a, dtype, ctas_of(sm_count), s);
     else launch_join<16>(a, dtype, ctas_of(sm_count), s);
 }
 

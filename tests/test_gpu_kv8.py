@@ -254,6 +254,26 @@ def test_attention_where_a_row_of_the_table_is_short(ctx, cols, page, rows, G):
     p.attend(q, [3, 0, 4, 2], cu, causal=False)
 
 
+@pytest.mark.parametrize("G,d,fmt,dtype", [(4, 128, 0, torch.float16), (1, 64, 1, torch.bfloat16), (9, 64, 0, torch.bfloat16),
+                                           (16, 128, 1, torch.float16), (17, 64, 0, torch.float16)])
+def test_attention_of_a_chunk_among_single_tokens(ctx, G, d, fmt, dtype):
+    """A prompt's chunk with sequences of a few rows: entries at both sides of every border between the kernels, padding, an empty sequence."""
+    p = Pair(ctx, pages=160, heads=2, page=32, d=d, fmt=fmt, seqs=24, cols=64, seed=3)
+    most = -(-512 // G) + 3
+    lens = [1, 2, 31, 32, 33, 127, 128, 129, 300, 700, 5, 64, 90, 200, 17, 3, 256, 40, 77, most + 150]
+    p.append(list(range(20)), lens)
+    counts = [1] * 11 + [max(1, 8 // G), 8 // G + 1, 16 // G + 1, 2, 1, 1, 0, 1, most]
+    seqs = list(range(20))
+    seqs[4] = -1
+    seqs.insert(9, 22)   # empty
+    counts.insert(9, 1)
+    cu = [sum(counts[:i]) for i in range(len(counts) + 1)]
+    q = torch.randn((cu[-1], 2 * G, d), generator=p.gen, device="cuda").to(dtype)
+    p.attend(q, seqs, cu)
+    p.attend(q, seqs, cu, window=50)
+    p.attend(q, seqs, cu, causal=False)
+
+
 @pytest.mark.parametrize("rows", [1, 40])
 def test_attention_over_a_long_cache(ctx, rows):
     """Many CTAs share a row tile; the whole call is one sequence's, or one long one's among short ones."""
