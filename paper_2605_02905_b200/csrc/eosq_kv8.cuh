@@ -104,7 +104,7 @@ struct Kv8Attend {
     Kv8 c;
     const int32_t *seqs, *cu;
     int n, max_q, G, causal, window;
-    int rows_min, rows_max;                    // entries of fewer or more rows than this are another launch's
+    int rows_min, rows_max;                    // entries of fewer or more rows than this are another launch's (or nobody's)
     int whole;                                 // row tiles are not shared between CTAs: a unit is one of them with a head
     long long total;
     const void *q;
@@ -116,13 +116,6 @@ struct Kv8Attend {
     float *part;                               // scratch: partial results, two slots per CTA
     int *err;
 };
-
-// Entry i of a call, with m = 0 where it is another launch's.
-__device__ __forceinline__ Kv8Seq kv8_seq(const Kv8Attend &a, int i) {
-    Kv8Seq s = kv8_seq(a.c, a.seqs, a.cu, i, a.total, a.max_q);
-    if (s.m * a.G < a.rows_min || s.m * a.G > a.rows_max) s.m = 0;
-    return s;
-}
 
 // The work of one call: every entry's query rows (query t, head g of a KV head: row t * G + g) cut into tiles of RT, the keys that
 // a row tile sees cut into tiles of KT.  A unit is one key tile of one row tile and KV head, or one of COST that stand for a row tile's beginning and
@@ -136,7 +129,10 @@ struct Kv8Tiles {
         hi = a.causal ? max(min(s.len, s.len - s.m + t1 + 1), 0) : s.len;
         lo = a.window > 0 ? max(s.len - s.m + t0 - a.window + 1, 0) : 0;
     }
-    static __device__ __forceinline__ int row_tiles(const Kv8Attend &a, const Kv8Seq &s) { return (s.m * a.G + RT - 1) / RT; }
+    static __device__ __forceinline__ int row_tiles(const Kv8Attend &a, const Kv8Seq &s) {
+        const int rows = s.m * a.G;
+        return (rows < a.rows_min || rows > a.rows_max) ? 0 : (rows + RT - 1) / RT;
+    }
     // Units of a row tile of so many key tiles and a head.
     static __device__ __forceinline__ int units(const Kv8Attend &a, int tiles) { return a.whole ? 1 : tiles + COST; }
     // First key tile of row tile r, and how many: at least one, so that rows which see nothing are written too.
@@ -168,7 +164,7 @@ struct Kv8Walk {
         if (left > 0) enter();
     }
     __device__ __forceinline__ void enter() {
-        s = kv8_seq(a, i);
+        s = kv8_seq(a.c, a.seqs, a.cu, i, a.total, a.max_q);
         row_tiles = (s.m > 0) ? T::row_tiles(a, s) : 0;
         r = 0;
     }
@@ -338,7 +334,7 @@ __device__ __forceinline__ Kv8Run kv8_run(const Kv8Attend &a, int *units) {
     __shared__ int total_units;
     const int tid = threadIdx.x;
     for (int i = tid; i < a.n; i += THREADS) {
-        const Kv8Seq s = kv8_seq(a, i);
+        const Kv8Seq s = kv8_seq(a.c, a.seqs, a.cu, i, a.total, a.max_q);
         int u = 0;
         if (s.m > 0) {
             const int tiles = T::row_tiles(a, s);
