@@ -274,6 +274,17 @@ def test_attention_of_a_chunk_among_single_tokens(ctx, G, d, fmt, dtype):
     p.attend(q, seqs, cu, causal=False)
 
 
+@pytest.mark.parametrize("counts,most", [([140, 5, 5, 3, 5, 5, 5, 4], None), ([1] * 150, 150), ([2, 0, 1] * 60, 400)])
+def test_attention_where_one_kernel_is_left_without_work(ctx, counts, most):
+    """A chunk among entries that are too long for the other kernel, and single tokens under a bound of a chunk's length."""
+    n = len(counts)
+    p = Pair(ctx, pages=2 * n + 40, heads=2, page=16, d=64, seqs=n, cols=40, seed=4)
+    p.append(list(range(n)), [max(c, 1) + 7 + i % 20 for i, c in enumerate(counts)])
+    cu = [sum(counts[:i]) for i in range(n + 1)]
+    q = torch.randn((cu[-1], 2 * 4, 64), generator=p.gen, device="cuda").half()
+    p.attend(q, list(range(n)), cu, most=most)
+
+
 @pytest.mark.parametrize("rows", [1, 40])
 def test_attention_over_a_long_cache(ctx, rows):
     """Many CTAs share a row tile; the whole call is one sequence's, or one long one's among short ones."""
