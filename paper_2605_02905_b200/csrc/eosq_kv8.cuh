@@ -282,6 +282,14 @@ struct Kv8Fetch {
 // the largest when m is exact.  x contains log2 of the page's value scale, so that the product with the codes of the values needs no
 // scaling; the sum of the weights takes it out again.
 constexpr float KV8_SHIFT = 6.0f, KV8_SLACK = 8.0f;
+// Base-2 logarithms beyond 2^22 are so far apart in fp32 that SHIFT - m, or a bound on them under one rounding, is off by whole powers of two of a weight: where a
+// maximum is that large, exponents are (x - m) + SHIFT, with x rounded as m was.  x - m is then exact where it matters, and no more than KV8_SLACK.
+__host__ __device__ __forceinline__ bool kv8_far(float m) { return fabsf(m) > 4194304.0f && m != -INFINITY; }
+// A maximum that only moves up, by whole powers of two, so that what has been rounded already is rescaled exactly.  (Where fp32 holds no fractions, the
+// sum may round to less than `top`, which is then itself a whole number away from m, or so far that nothing is left of what was there.)
+__host__ __device__ __forceinline__ float kv8_moved(float m, float top) {
+    return (m == -INFINITY) ? top : fmaxf(m + ceilf(fmaxf(top - m, 0.0f)), top);
+}
 __device__ __forceinline__ float exp2_fast(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));

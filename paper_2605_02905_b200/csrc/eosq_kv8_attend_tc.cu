@@ -186,10 +186,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
                     unpair(sum, s0, s1);
                     return s0 + s1;
                 };
-                // A new maximum, for the sum and for the sums of values (the products that made them have ended: the scores came behind them).  A maximum only moves up,
-                // by whole powers of two, so that what has been rounded already is rescaled exactly.
+                // A new maximum, for the sum and for the sums of values (the products that made them have ended: the scores came behind them).
                 auto move = [&](float top) {
-                    const float to = (m == -INFINITY) ? top : m + ceilf(fmaxf(top - m, 0.0f)), by = (to == -INFINITY) ? 1.0f : exp2_fast(m - to);
+                    const float to = kv8_moved(m, top), by = (to == -INFINITY) ? 1.0f : exp2_fast(m - to);
                     m = to;
                     l *= by;
                     if (!first) {
@@ -208,75 +207,71 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
                 // where it can be.  Four prompts of 500 to 2048 queries on up to 12000 tokens, and four of 2048 on 12000: two passes in loops of 32 tokens, twice unrolled,
                 // 745 and 1879 us; of 16 tokens 635 and 1687; one pass of 16 tokens 638 and 1662, of 32 634 and 1524, of 64 629 and 1458.
                 constexpr int TURN = 4;   // in sixteens
-                if (first || edge || __any_sync(0xffffffffu, m == -INFINITY || fabsf(m) > 4194304.0f)) {
-                    // With a look at all scores before the first weight: a row tile's first tile, masks, rows that have seen nothing yet; and logarithms so large that
-                    // s * ks + (vlog - m + shift), which is rounded once, could pass fp16's range where m was rounded before: there every one is rounded as m was.
+                const bool look = first || edge || __any_sync(0xffffffffu, m == -INFINITY || kv8_far(m));
+                int done = 0;   // sixteens whose weights have been made
+                if (!look) {
+                    // Under the maximum so far.  Where the weights of a turn add up to no more than 2^14 none is beyond fp16's range, nor is the maximum more than KV8_SLACK behind; else, which
+                    // is rare, this turn and what is left of the tile is looked at first.
+#pragma unroll 1
+                    for (; done < GROUPS; done += TURN) {
+                        uint32_t y[TURN][GROUP], q[TURN][GROUP / 2];
+#pragma unroll
+                        for (int i = 0; i < TURN; ++i) tmem_ld16(s_at + GROUP * (done + i), y[i]);
+                        float sum = 0.0f, add = 0.0f;
+#pragma unroll
+                        for (int i = 0; i < TURN; ++i) {
+                            const float kf = ks_of(done + i), cf = ti.vlog[done + i] + KV8_SHIFT;
+                            tmem_ld_wait(y[i]);
+                            const float s16 = weights(y[i], q[i], kf, cf - m);
+                            sum += s16;
+                            add = fmaf(s16, ti.vinv[done + i], add);
+                        }
+                        if (__any_sync(0xffffffffu, sum > 16384.0f)) break;   // (not for a NaN, which stays one)
+                        l += add;
+#pragma unroll
+                        for (int i = 0; i < TURN; ++i) tmem_st8(s_at + GROUP / 2 * (done + i), q[i]);   // in the place of scores that have been read
+                    }
+                }
+                if (done < GROUPS) {
+                    // With a look at all scores that are left before the next weight: a row tile's first tile, masks, rows that have seen nothing yet; a turn whose weights were too
+                    // large; and logarithms beyond kv8_far's bound.  Whatever the scores are, each is looked at once and then weighed once.
                     float top = -INFINITY;
 #pragma unroll 1
-                    for (int g = 0; g < GROUPS; ++g) {
+                    for (int g = done; g < GROUPS; ++g) {
                         read(g);
                         if (edge) hide(g);
                         top = fmaxf(top, largest(g));
                     }
-                    if (__any_sync(0xffffffffu, top > m + KV8_SLACK)) move(top);
-                    const bool far = __any_sync(0xffffffffu, fabsf(m) > 4194304.0f && m != -INFINITY);
-                    const float b = (m == -INFINITY) ? 0.0f : KV8_SHIFT - m;
+                    if (__any_sync(0xffffffffu, top - m > (look ? KV8_SLACK : 0.0f))) {
+                        const __half2 by = __float2half2_rn(move(top));
 #pragma unroll 1
-                    for (int g = 0; g < GROUPS; ++g) {
+                        for (int i = 0; i < done; ++i) {   // the weights before these
+                            tmem_ld8(s_at + GROUP / 2 * i, p);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int e = 0; e < GROUP / 2; ++e) {
+                                const __half2 v = __hmul2(*reinterpret_cast<const __half2 *>(&p[e]), by);
+                                p[e] = *reinterpret_cast<const uint32_t *>(&v);
+                            }
+                            tmem_st8(s_at + GROUP / 2 * i, p);
+                        }
+                    }
+                    const bool mine_far = kv8_far(m), far = __any_sync(0xffffffffu, mine_far);   // (a row's arithmetic goes by its own maximum)
+                    const float m0 = (m == -INFINITY) ? 0.0f : m, b = KV8_SHIFT - m0;
+#pragma unroll 1
+                    for (int g = done; g < GROUPS; ++g) {
                         read(g);
                         if (edge) hide(g);
-                        float kf = ks_of(g), cf = ti.vlog[g];
+                        float kf = ks_of(g), cf = ti.vlog[g] + b;
                         if (far) {
 #pragma unroll
-                            for (int e = 0; e < GROUP; ++e) x[e] = __float_as_uint(fmaf(__uint_as_float(x[e]), kf, cf));
-                            kf = 1.0f;
-                            cf = 0.0f;
+                            for (int e = 0; e < GROUP; ++e)
+                                if (mine_far) x[e] = __float_as_uint(fmaf(__uint_as_float(x[e]), kf, ti.vlog[g]) - m0);
+                            kf = mine_far ? 1.0f : kf;
+                            cf = mine_far ? KV8_SHIFT : cf;
                         }
-                        l = fmaf(weights(x, p, kf, cf + b), ti.vinv[g], l);
+                        l = fmaf(weights(x, p, kf, cf), ti.vinv[g], l);
                         tmem_st8(s_at + GROUP / 2 * g, p);   // in the place of scores that have been read
-                    }
-                } else {
-                    // Under the maximum so far.  Where the weights of a turn add up to no more than 2^14 none is beyond fp16's range, nor is the maximum more than KV8_SLACK behind; else, which
-                    // is rare, it is moved and they are made again.
-#pragma unroll 1
-                    for (int g = 0; g < GROUPS; g += TURN) {
-                        uint32_t y[TURN][GROUP], q[TURN][GROUP / 2];
-#pragma unroll
-                        for (int i = 0; i < TURN; ++i) tmem_ld16(s_at + GROUP * (g + i), y[i]);
-                        float sum = 0.0f, add = 0.0f;
-#pragma unroll
-                        for (int i = 0; i < TURN; ++i) {
-                            const float kf = ks_of(g + i), cf = ti.vlog[g + i] + KV8_SHIFT;
-                            tmem_ld_wait(y[i]);
-                            const float s16 = weights(y[i], q[i], kf, cf - m);
-                            sum += s16;
-                            add = fmaf(s16, ti.vinv[g + i], add);
-                        }
-                        if (__any_sync(0xffffffffu, sum > 16384.0f)) {   // (not for a NaN, which stays one)
-                            float top = -INFINITY;
-#pragma unroll 1
-                            for (int i = g; i < g + TURN; ++i) {
-                                read(i);
-                                top = fmaxf(top, largest(i));
-                            }
-                            const __half2 by = __float2half2_rn(move(top));
-#pragma unroll 1
-                            for (int i = 0; i < g; ++i) {   // the weights before these
-                                tmem_ld8(s_at + GROUP / 2 * i, p);
-                                tmem_ld_wait();
-#pragma unroll
-                                for (int e = 0; e < GROUP / 2; ++e) {
-                                    const __half2 v = __hmul2(*reinterpret_cast<const __half2 *>(&p[e]), by);
-                                    p[e] = *reinterpret_cast<const uint32_t *>(&v);
-                                }
-                                tmem_st8(s_at + GROUP / 2 * i, p);
-                            }
-                            g -= TURN;
-                            continue;
-                        }
-                        l += add;
-#pragma unroll
-                        for (int i = 0; i < TURN; ++i) tmem_st8(s_at + GROUP / 2 * (g + i), q[i]);   // in the place of scores that have been read
                     }
                 }
                 tmem_st_wait();
