@@ -243,6 +243,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
                         top = fmaxf(top, largest(g));
                     }
                     if (__any_sync(0xffffffffu, top - m > (look ? KV8_SLACK : 0.0f))) {
+                        if (done) tmem_st_wait();   // weights that are read again below have been stored: nothing else orders a load behind a store to tensor memory
                         const __half2 by = __float2half2_rn(move(top));
 #pragma unroll 1
                         for (int i = 0; i < done; ++i) {   // the weights before these
