@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
         // Rows of the row tile `tile_of`: query and head (row - query * G) of the one that this lane loads, and of the two that it holds weights of.
         int tile_of = -1, t_load[NB], h_load[NB], t_row[NB][2], h_row[NB][2];
         uint32_t items = 0;
-        bool ok = true;
+        bool ok = true, far = false;   // far: some row's maximum is (kv8_far)
         for (uint32_t it = 0;; ++it) {
             const int st = it % STAGES;
             ok = mbar_wait_warp(&full_bar[st], (it / STAGES) & 1u, &abort_flag);
@@ -205,6 +205,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
             if (ti.first) {
                 const Kv8Seq sq{0, ti.len, mq, 0};
                 const int r = ti.r;
+                far = false;
                 if (r != tile_of) {
                     tile_of = r;
 #pragma unroll
@@ -307,8 +308,9 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) moved |= top[n][e] > m[n][e] + KV8_SLACK;
+                    for (int e = 0; e < 2; ++e) moved |= top[n][e] - m[n][e] > KV8_SLACK;   // (of two minus infinities: no)
                 if (__any_sync(0xffffffffu, moved)) {
+                    bool mine_far = false;
 #pragma unroll
                     for (int n = 0; n < NB; ++n) {
 #pragma unroll
@@ -319,6 +321,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
                             t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
                             const float to = fmaxf(m[n][e], t), by = (to == -INFINITY) ? 1.0f : exp2_fast(m[n][e] - to);
                             m[n][e] = to;
+                            mine_far |= kv8_far(to);
                             l[n][e] *= by;
 #pragma unroll
                             for (int b = 0; b < 2 * WORDS; ++b) {
@@ -327,15 +330,30 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
                             }
                         }
                     }
+                    far = __any_sync(0xffffffffu, mine_far);
                 }
                 uint32_t pb[SHARE][NB][2];
 #pragma unroll
                 for (int n = 0; n < NB; ++n) {
-                    const float b0 = (m[n][0] == -INFINITY) ? 0.0f : KV8_SHIFT - m[n][0], b1 = (m[n][1] == -INFINITY) ? 0.0f : KV8_SHIFT - m[n][1];
+                    float b[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) b[e] = (m[n][e] == -INFINITY) ? 0.0f : KV8_SHIFT - m[n][e];
+                    if (far) {   // (a row's arithmetic goes by its own maximum)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            if (kv8_far(m[n][e])) {
+#pragma unroll
+                                for (int p = 0; p < SHARE; ++p) {
+                                    sc[p][n][e] -= m[n][e];
+                                    sc[p][n][2 + e] -= m[n][e];
+                                }
+                                b[e] = KV8_SHIFT;
+                            }
+                    }
 #pragma unroll
                     for (int p = 0; p < SHARE; ++p) {
-                        const float p0 = exp2_fast(sc[p][n][0] + b0), p1 = exp2_fast(sc[p][n][1] + b1);
-                        const float p2 = exp2_fast(sc[p][n][2] + b0), p3 = exp2_fast(sc[p][n][3] + b1);
+                        const float p0 = exp2_fast(sc[p][n][0] + b[0]), p1 = exp2_fast(sc[p][n][1] + b[1]);
+                        const float p2 = exp2_fast(sc[p][n][2] + b[0]), p3 = exp2_fast(sc[p][n][3] + b[1]);
                         const float vinv = ti.vinv[warp * SHARE + p];
                         l[n][0] = fmaf(p0 + p2, vinv, l[n][0]);
                         l[n][1] = fmaf(p1 + p3, vinv, l[n][1]);

@@ -74,7 +74,7 @@ def _hold(ctx, p, q, n, sign=1, **kw):
     assert (np.abs(lg - z) <= 2.0 ** -22 * np.abs(z) + 2.0 ** -18).all()
 
 
-@pytest.mark.parametrize("rows", [150])
+@pytest.mark.parametrize("rows", [1, 4, 150])
 @pytest.mark.parametrize("fmt,d,dtype", [(0, 128, "f16"), (1, 64, "bf16")])
 @pytest.mark.parametrize("power", [4, 8, 16, 20, 22, 24, 25, 26, 27, 28, 30, 33, 36, 44, 60, 80])
 def test_logits_that_become_large_in_a_later_tile(ctx, power, fmt, d, dtype, rows):
@@ -91,7 +91,7 @@ def test_logits_that_become_large_in_a_later_tile(ctx, power, fmt, d, dtype, row
     _hold(ctx, p, q, n, window=400)
 
 
-@pytest.mark.parametrize("rows", [150])
+@pytest.mark.parametrize("rows", [1, 4, 150])
 @pytest.mark.parametrize("fmt,d,dtype", [(0, 64, "bf16"), (1, 128, "f16")])
 @pytest.mark.parametrize("power", range(-4, 9))
 def test_large_logits_close_to_one_another(ctx, power, fmt, d, dtype, rows):
