@@ -277,6 +277,10 @@ struct Kv8Fetch {
     }
 };
 
+// A bf16 row is divided by 2^e, which brings its largest value to 2^14 .. 2^15 (a row of less than 2^-112: to less).  These are all exponents that finite rows can have
+// there; 2^e and 2^-e are normal numbers.
+constexpr int KV8_EXP_MIN = -126, KV8_EXP_MAX = 113;
+
 // Scores are base-2 logarithms; a weight is 2^(x - m + KV8_SHIFT), m being a running maximum that is only moved when a score passes
 // it by more than KV8_SLACK.  So weights are at most 2^14, inside fp16, and those of fp16's smallest normal numbers are 2^-20 of
 // the largest when m is exact.  x contains log2 of the page's value scale, so that the product with the codes of the values needs no

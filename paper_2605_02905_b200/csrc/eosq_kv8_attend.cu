@@ -75,7 +75,7 @@ __device__ __forceinline__ float query_row(const void *p, uint32_t (&v)[NQ / 2],
     for (int i = 0; i < NQ / 2; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(v[i] << 16)), fabsf(__uint_as_float(v[i] & 0xffff0000u))));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const int e = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 14, -100), 100);
+    const int e = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 14, KV8_EXP_MIN), KV8_EXP_MAX);
     const float f = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
 #pragma unroll
     for (int i = 0; i < NQ / 2; ++i) v[i] = half2_bits(__uint_as_float(v[i] << 16) * f, __uint_as_float(v[i] & 0xffff0000u) * f);
@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
         Kv8Batch next = fetch.next();
         while (ok && now.tiles) {
             Kv8Batch after = next;
-            const float ks = now.ks * a.scale_log2;
+            const float ks = BF16 ? now.ks : now.ks * a.scale_log2;   // (with bf16 the scale goes with the row's power of two first, which it may well cancel)
             const float vs = fminf(fmaxf(now.vs, KV8_SCALE_MIN), KV8_SCALE_MAX);
             const float vlog = now.page >= 0 ? log2f(vs) : -INFINITY, vinv = 1.0f / vs;
             int row;
@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv8_rows_kernel(const __
                     }
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        f[n][e] = BF16 ? __shfl_sync(0xffffffffu, mine, (2 * q + e) * 4) : 1.0f;
+                        f[n][e] = BF16 ? __shfl_sync(0xffffffffu, mine, (2 * q + e) * 4) * a.scale_log2 : 1.0f;
                         lo[n][e] = hi[n][e] = 0;
                         if (t_row[n][e] < mq) Tiles::span(a, sq, t_row[n][e], t_row[n][e], lo[n][e], hi[n][e]);
                         m[n][e] = -INFINITY;

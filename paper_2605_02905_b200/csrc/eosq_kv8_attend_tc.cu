@@ -531,7 +531,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_tiles_kernel(const __grid_cons
                             }
                             top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 1));
                             top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                            const int e2 = min(max(static_cast<int>(max(top >> 16, top & 0xffffu) >> 7) - 127 - 14, -100), 100);
+                            const int e2 = min(max(static_cast<int>(max(top >> 16, top & 0xffffu) >> 7) - 127 - 14, KV8_EXP_MIN), KV8_EXP_MAX);
                             g = __uint_as_float(static_cast<uint32_t>(127 - e2) << 23);
                             if ((lane & 3) == 0) q_exp[items & 1][half * HALF + at] = static_cast<int8_t>(e2);
                         }

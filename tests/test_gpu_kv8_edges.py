@@ -1,0 +1,37 @@
+"""The 8-bit paged cache on the GPU at the edges of what its calls take."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_02905_b200 as eosq
+from test_gpu_kv8 import Pair, _ints
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = eosq.Context()
+    yield c
+    c.close()
+
+
+@pytest.mark.parametrize("fmt,d", [(0, 128), (1, 64)])
+@pytest.mark.parametrize("rows", [3, 40])
+def test_bf16_queries_from_the_smallest_to_the_largest(ctx, fmt, d, rows):
+    """Rows whose largest value is anything that bf16 holds, under a scale that brings the logits back: each is held to fp16's precision by its own power of two."""
+    p = Pair(ctx, pages=30, heads=1, page=16, d=d, fmt=fmt, seqs=2, cols=20, seed=1)
+    p.append([0], [100], "f32")
+    base = torch.randn((rows, 5, d), generator=p.gen, device="cuda").clamp(-3, 3)
+    for power in (127, 126, 120, 117, 116, 115, 114, 113, 100, -100, -112, -113, -120, -126, -130):
+        q = (base.double() * 2.0 ** (power - 2)).bfloat16()      # the largest is 2^-1 .. 3 of 2^(power - 2)
+        assert bool(torch.isfinite(q).all()) and float(q.abs().max()) > 0
+        q[0, 1] = q[0, 1] * 2.0 ** -60 if power > 0 else q[0, 1]     # small rows, and none, beside them
+        q[1, 2] = 0.0
+        p.attend(q, [0], [0, rows], scale=2.0 ** -max(min(power, 120), -120))
+        p.attend(q, [0], [0, rows], scale=-(2.0 ** -max(min(power, 120), -120)), causal=False)
+    top = torch.finfo(torch.bfloat16).max
+    q = torch.full((rows, 5, d), top, device="cuda").bfloat16() * torch.sign(base).bfloat16()
+    p.attend(q, [0], [0, rows], scale=1e-39)
