@@ -70,8 +70,9 @@ int entry(F &&f) {
     }
 }
 
+// A fork's plan (lists with padding may be longer than the cache has sequences), a compaction's moves.
 size_t pages_scratch(const eosq_kv8_t *c) {
-    return std::max(sizeof(int2) * static_cast<size_t>(c->max_seqs), sizeof(int32_t) * (64 + static_cast<size_t>(c->num_pages)));
+    return std::max(sizeof(int2) * static_cast<size_t>(EOSQ_KV8_MAX_SEQS), sizeof(int32_t) * (64 + static_cast<size_t>(c->num_pages)));
 }
 size_t kv8_attend_scratch(int64_t most, int d) { return most <= 16 ? kv8_rows_scratch(d) : std::max(kv8_rows_scratch(d), kv8_tiles_scratch(d)); }
 size_t cuts_scratch() { return align_up(sizeof(Kv8Cut) * KV8_MAX_CTAS, 256); }
@@ -208,7 +209,7 @@ extern "C" int eosq_kv8_fork(eosq_ctx *ctx, const eosq_kv8_t *cache, const int32
         Kv8 c;
         if (!ctx || n < 0) return EOSQ_ERR_INVALID_ARG;
         if (int rc = view_of(cache, 0, &c)) return rc;
-        if (n > c.max_seqs || static_cast<int64_t>(n) * c.layers * 2 * ((c.page_bytes() >> 14) + 1) >= (int64_t(1) << 31)) return EOSQ_ERR_UNSUPPORTED;
+        if (n > EOSQ_KV8_MAX_SEQS || static_cast<int64_t>(n) * c.layers * 2 * ((c.page_bytes() >> 14) + 1) >= (int64_t(1) << 31)) return EOSQ_ERR_UNSUPPORTED;
         if (n == 0) return EOSQ_OK;
         if (!list_ok(src) || !list_ok(dst) || !workspace || misaligned(workspace, 255)) return EOSQ_ERR_INVALID_ARG;
         if (workspace_bytes < pages_scratch(cache)) return EOSQ_ERR_BUFFER_TOO_SMALL;

@@ -35,3 +35,15 @@ def test_bf16_queries_from_the_smallest_to_the_largest(ctx, fmt, d, rows):
     top = torch.finfo(torch.bfloat16).max
     q = torch.full((rows, 5, d), top, device="cuda").bfloat16() * torch.sign(base).bfloat16()
     p.attend(q, [0], [0, rows], scale=1e-39)
+
+
+def test_fork_with_a_padded_list(ctx):
+    """More entries than the cache has sequences, most of them padding: the others are served as in a short list."""
+    p = Pair(ctx, layers=2, pages=30, heads=2, page=16, d=64, seqs=6, cols=6, seed=3)
+    p.append([0, 1], [40, 17])
+    src, dst = [-1] * 700, [-1] * 700
+    for i, a, b in ((3, 0, 2), (40, 1, 4), (41, -1, 5), (500, 0, -1), (698, 1, 3)):
+        src[i], dst[i] = a, b
+    eosq.eosq_kv8_fork(ctx, p.c, _ints(src), _ints(dst))
+    p.m.fork(src, dst)
+    p.same()

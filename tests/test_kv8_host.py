@@ -140,3 +140,12 @@ def test_the_oracle_knows_the_formats():
     assert o.encode(0, np.array([0.5, 1.5, -2.5, 126.5, 127.49, -300.0, np.nan, np.inf])).view(np.int8).tolist() == [0, 2, -2, 126, 127, -127, 0, 127]
     assert o.scale_of(1, 448.0) == 1.0 and o.scale_of(1, np.nextafter(448.0, 500)) == 2.0 and o.scale_of(1, 224.0) == 0.5 and o.scale_of(1, 0.0) == 2.0 ** -64
     assert o.scale_of(0, 127.0) == 1.0 and o.scale_of(0, 0.0) == 2.0 ** -64 and o.scale_of(0, 3e38) == 2.0 ** 64
+
+
+def test_a_padded_list_to_fork():
+    """A call's list may be longer than the cache has sequences (entries of -1 are padding), in fork as in the other calls: up to the workspace, nothing refuses it."""
+    c = _cache(max_seqs=8)
+    for n in (9, 100, 8192):
+        assert _calls(c, n=n, wsb=255)["fork"]() == SMALL
+    need = eosq.lib().eosq_kv8_workspace_bytes(ctypes.pointer(c), 0)
+    assert need >= 8 * 8192 and _calls(c, n=9, wsb=need - 256)["fork"]() == SMALL
