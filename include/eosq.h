@@ -295,7 +295,8 @@ int eosq_kv8_attend(eosq_ctx *ctx, const eosq_kv8_t *cache, int layer, const voi
 /*
  * Sequence dst[i] becomes a copy of sequence src[i] as it was before the call, i = 0 .. n-1 (dev int32 arrays): they share its whole pages, a last page
  * that is not full is copied, in all layers, to the lowest free page.  A destination is empty and listed once (else the entry is
- * refused and raises a flag: it stays empty); a source may be listed more than once.
+ * refused and raises a flag: it stays empty); a source may be listed more than once.  Where a source's table names a page outside the pool the copy's names
+ * none (and a flag is raised).
  */
 int eosq_kv8_fork(eosq_ctx *ctx, const eosq_kv8_t *cache, const int32_t *src, const int32_t *dst, int n, void *workspace,
                   size_t workspace_bytes, void *cuda_stream);

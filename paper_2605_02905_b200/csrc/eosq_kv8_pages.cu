@@ -246,17 +246,20 @@ __global__ void __launch_bounds__(COPY_THREADS) kv8_fork_copy_kernel(const Kv8 c
             to[col] = p;
             atomicAdd(&c.refs[p], 1);
         }
-        if (threadIdx.x == 0) {
-            if (tail) to[full] = plan[i].y;
-            c.lengths[dst[i]] = len;
-        }
+        if (threadIdx.x == 0) c.lengths[dst[i]] = len;
     }
     if (!tail) return;
     const int p = from[full];
-    if (p < 0 || p >= c.num_pages) {
-        if (threadIdx.x == 0) raise(c, EOSQ_KV8_BAD_PAGE);
-        return;
+    const bool there = p >= 0 && p < c.num_pages;
+    if (q == 0 && threadIdx.x == 0) {
+        if (there) {
+            to[full] = plan[i].y;
+        } else {   // nothing to copy: the page that was taken for it is free again, and the copy's entry is none, as its other ones outside the pool are
+            c.refs[plan[i].y] = 0;
+            raise(c, EOSQ_KV8_BAD_PAGE);
+        }
     }
+    if (!there) return;
     copy_piece(c, c, p, plan[i].y, q / (2 * pieces), (q / pieces) & 1, q % pieces);
 }
 

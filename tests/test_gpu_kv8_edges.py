@@ -47,3 +47,34 @@ def test_fork_with_a_padded_list(ctx):
     eosq.eosq_kv8_fork(ctx, p.c, _ints(src), _ints(dst))
     p.m.fork(src, dst)
     p.same()
+
+
+@pytest.mark.parametrize("bad", [-1, 30, 2 ** 31 - 1])
+def test_fork_of_a_sequence_with_a_page_outside_the_pool(ctx, bad):
+    """A whole page, or the last one, which would be copied: the copy names none there, counts add up, and a page taken for a copy is free again."""
+    for col in (0, 2):
+        p = Pair(ctx, layers=2, pages=30, heads=2, page=16, d=64, seqs=6, cols=6, seed=3)
+        p.append([0, 1], [40, 17])
+        p.same()
+        good = int(p.c.table[0, col])
+        p.c.table[0, col] = bad
+        eosq.eosq_kv8_fork(ctx, p.c, _ints([0, 1]), _ints([2, 3]))
+        assert eosq.eosq_kv8_check(ctx, p.c) == eosq.EOSQ_KV8_BAD_PAGE
+        p.m.fork([0, 1], [2, 3])
+        if col == 2:
+            p.m.refs[p.m.table[2, col]] = 0
+            for x in p.m.code + p.m.scale:   # (nothing was copied there)
+                x[:, p.m.table[2, col]] = 0
+        else:
+            p.m.refs[good] -= 1
+        taken = int(p.m.table[2, col])
+        p.m.table[2, col] = -1
+        p.c.table[0, col] = good
+        if col == 2:
+            for x in (p.c.k, p.c.v, p.c.k_scale, p.c.v_scale):
+                x[:, taken] = 0
+        p.same()
+        eosq.eosq_kv8_free(ctx, p.c, _ints([2, 3, 0, 1]))
+        p.m.free([2, 3, 0, 1])
+        p.same()
+        assert int(p.c.refs.sum()) == 0
