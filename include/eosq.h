@@ -283,7 +283,8 @@ int eosq_kv8_store(eosq_ctx *ctx, const eosq_kv8_t *cache, int layer, const void
  *   max_q   host, at least the largest cu[i+1] - cu[i]; an entry with more is skipped.  EOSQ_ERR_UNSUPPORTED where total * G / (8, 16 or
  *           256 rows) * kv_heads * (positions of a table row / 128) reaches 2^31
  *   workspace  eosq_kv8_workspace_bytes(cache, max_q*G)
- * Rows that belong to no entry (behind cu[n], or of a sequence of -1) are left as they are.  Sums and the statistics are held in fp32;
+ * Offsets ascend, over skipped entries too, so that rows belong to one entry.  Rows that belong to no entry (behind cu[n], or of a sequence of -1) are
+ * left as they are.  Sums and the statistics are held in fp32;
  * weights are rounded to fp16 before they meet the values.  `lse` lets a caller join the result with attention over other tokens
  * of the sequence.
  */

@@ -304,7 +304,9 @@ __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// Exclusive prefix sums of units[0 .. n) in place, by one warp; the total.
+// Exclusive prefix sums of units[0 .. n) in place, by one warp; the total, or KV8_TOO_MANY where it is as much or more (the sums are of no use then).
+constexpr int KV8_TOO_MANY = 0x7fffffff;
+__device__ __forceinline__ int sum_of(int a, int b) { return static_cast<int>(min(static_cast<unsigned>(a) + static_cast<unsigned>(b), static_cast<unsigned>(KV8_TOO_MANY))); }
 __device__ __forceinline__ int warp_prefix(int *units, int n) {
     const int lane = threadIdx.x & 31;
     int total = 0;
@@ -314,10 +316,10 @@ __device__ __forceinline__ int warp_prefix(int *units, int n) {
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, x, o);
-            if (lane >= o) x += y;
+            if (lane >= o) x = sum_of(x, y);
         }
-        if (base + lane < n) units[base + lane] = total + x - v;
-        total += __shfl_sync(0xffffffffu, x, 31);
+        if (base + lane < n) units[base + lane] = sum_of(total, x - v);
+        total = sum_of(total, __shfl_sync(0xffffffffu, x, 31));
     }
     return total;
 }
@@ -357,7 +359,11 @@ __device__ __forceinline__ Kv8Run kv8_run(const Kv8Attend &a, int *units) {
     }
     __syncthreads();
     if (tid < 32) {
-        const int t = warp_prefix(units, a.n);
+        int t = warp_prefix(units, a.n);
+        if (t == KV8_TOO_MANY) {   // more than all rows can have (the entry point's bound): offsets go back, and rows are counted many times over
+            t = 0;
+            if (tid == 0) raise(a.c, EOSQ_KV8_BAD_SEQ);
+        }
         if (tid == 0) total_units = t;
     }
     __syncthreads();
