@@ -81,14 +81,15 @@ def test_fork_of_a_sequence_with_a_page_outside_the_pool(ctx, bad):
 
 
 def test_offsets_that_go_back_over_and_over(ctx):
-    """Between entries of padding every entry claims all rows again: 4096 x 2500 row tiles x 130 units x 2 heads are 2.7e9, which 32 bits do not hold (the bound on
+    """Between entries of padding every entry claims all rows again: 4096 x 32 row tiles x 1026 units x 20 heads are 2.7e9, which 32 bits do not hold (the bound on
     a call's units goes by its rows).  Nothing is done, and a flag says so; the next call is answered."""
-    n, total = 8192, 10000
-    p = Pair(ctx, pages=130, heads=2, page=128, d=64, seqs=2, cols=128, seed=3)
-    p.append([0], [128 * 128])
-    q = torch.randn((total, 8, 64), generator=p.gen, device="cuda").half()
+    n, total = 8192, 511
+    p = Pair(ctx, pages=1030, heads=20, page=128, d=64, seqs=2, cols=1024, seed=3)
+    p.reserve([0], [1024 * 128])
+    p.append([1], [200])
+    q = torch.randn((total, 20, 64), generator=p.gen, device="cuda").half()
     out = torch.full_like(q, 3.0)
     seqs, cu = _ints([0, -1] * (n // 2)), _ints([0, total] * (n // 2) + [0])
     eosq.eosq_kv8_attend(ctx, p.c, 0, q, seqs, cu, total, causal=False, out=out)
     assert eosq.eosq_kv8_check(ctx, p.c) == eosq.EOSQ_KV8_BAD_SEQ and bool((out == 3.0).all())
-    p.attend(q[:3], [0], [0, 3])
+    p.attend(q[:3], [1], [0, 3])
