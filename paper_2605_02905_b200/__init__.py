@@ -448,11 +448,11 @@ def _kv8_list(cache, t, n, what):
 
 
 def _kv8_rows(cache, t, heads, what):
-    """Data pointer and strides of [total][heads][d], d contiguous."""
+    """Data pointer and strides of [total][heads][d], d contiguous; 0 for the stride of a dimension of one, which torch gives any value."""
     stride = t.stride()
     if len(stride) != 3 or stride[2] != 1 or t.size(1) != heads or t.size(2) != cache.d or t.get_device() != cache._index:
         raise ValueError(f"{what}: [total][{heads}][{cache.d}] with contiguous rows on {cache.device} is wanted, not {list(t.shape)} on {t.device}")
-    return t.data_ptr(), stride[0], stride[1]
+    return t.data_ptr(), stride[0] if t.size(0) > 1 else 0, stride[1] if heads > 1 else 0
 
 
 def _any_dtype_code(t):

@@ -93,3 +93,17 @@ def test_offsets_that_go_back_over_and_over(ctx):
     eosq.eosq_kv8_attend(ctx, p.c, 0, q, seqs, cu, total, causal=False, out=out)
     assert eosq.eosq_kv8_check(ctx, p.c) == eosq.EOSQ_KV8_BAD_SEQ and bool((out == 3.0).all())
     p.attend(q[:3], [1], [0, 3])
+
+
+def test_dimensions_of_one_with_any_stride(ctx):
+    """One token, or one head, whose stride is no multiple of 16 bytes: torch calls such a tensor contiguous, and the stride is never used."""
+    p = Pair(ctx, pages=12, heads=1, page=16, d=64, seqs=2, cols=6, seed=3)
+    odd = lambda n, dtype=torch.float16: torch.randn((n, 1, 64), generator=p.gen, device="cuda").to(dtype).as_strided((n, 1, 64), (64 if n > 1 else 65, 1, 1))
+    assert odd(1).is_contiguous() and odd(1).stride() == (65, 1, 1)
+    for n in (1, 20):
+        p.store(0, odd(n), odd(n), [0], p.reserve([0], [n]), [0, n])
+    p.same()
+    for n in (1, 5):
+        q = odd(n)
+        out = torch.empty((n, 1, 64), dtype=torch.float16, device="cuda").as_strided((n, 1, 64), q.stride())
+        p.attend(q, [0], [0, n], out=out)
