@@ -103,3 +103,23 @@ def test_large_logits_close_to_one_another(ctx, power, fmt, d, dtype, rows):
         q = _queries(dtype, rows, 3, d, factors, 0, power + 50)
         _hold(ctx, p, q, n)
         _hold(ctx, p, q, n, causal=False, sign=-1)
+
+
+@pytest.mark.parametrize("rows", [1, 4, 150])
+@pytest.mark.parametrize("fmt,d,dtype", [(0, 128, "f16"), (1, 64, "bf16"), (0, 64, "f16"), (1, 128, "bf16")])
+@pytest.mark.parametrize("way", ["up", "down", "up_and_down", "steps", "at_random"])
+def test_maxima_that_move_often(ctx, way, fmt, d, dtype, rows):
+    """Logits of ordinary size that grow from page to page, by less and by more than the slack, so that maxima move at a tile's beginning, in its middle, under weights
+    that have been made already, and in many tiles of a row tile; that become smaller again, so that nothing later counts; and any mixture."""
+    n, g = 900, np.random.RandomState(7)
+    pages = -(-n // 16)
+    at = np.arange(pages) / pages
+    powers = np.floor({"up": -6 + 18 * at, "down": 12 - 18 * at, "up_and_down": 12 - 36 * np.abs(at - 0.5), "steps": np.where(np.arange(pages) % 8 < 5, -4, -4 + 16 * at),
+                       "at_random": g.uniform(-6, 12, pages)}[way]).astype(int)
+    level = np.where(g.rand(n) < 0.3, g.randint(-3, 4, n), 0)
+    p = _cache(ctx, fmt, d, level, g.randint(-8, 9, n), powers, 3)
+    q = _queries(dtype, rows, 3, d, [2, -2, 1, 0], 3, 5)
+    _hold(ctx, p, q, n)
+    _hold(ctx, p, q, n, causal=False)
+    _hold(ctx, p, q, n, sign=-1)
+    _hold(ctx, p, q, n, window=500)
