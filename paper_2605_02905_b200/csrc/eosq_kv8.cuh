@@ -505,7 +505,7 @@ constexpr int KV8_COST_BOUND = 5;   // no kernel counts a row tile's beginning a
 
 // ---- launchers ------------------------------------------------------------------------------------
 void launch_kv8_store(const Kv8 &c, int fmt, const void *const (&x)[2], int dtype, long long total, const long long (&tok)[2],
-                      const long long (&head)[2], const int32_t *seqs, const int32_t *first, const int32_t *cu, int n, int max_new, cudaStream_t s);
+                      const long long (&head)[2], const int32_t *seqs, const int32_t *first, const int32_t *cu, int n, int max_new, int sm_count, cudaStream_t s);
 bool launch_kv8_reserve(const Kv8 &c, const int32_t *seqs, const int32_t *add, int n, int32_t *first, cudaStream_t s);
 bool launch_kv8_fork(const Kv8 &c, const int32_t *src, const int32_t *dst, int n, int2 *plan, cudaStream_t s);
 void launch_kv8_fork_copy(const Kv8 &c, const int32_t *src, const int32_t *dst, int n, const int2 *plan, cudaStream_t s);

@@ -127,7 +127,7 @@ extern "C" int eosq_kv8_store(eosq_ctx *ctx, const eosq_kv8_t *cache, int layer,
         cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
         run_stage(ctx, ST_OTHER, s, [&] {
             launch_kv8_store(c, cache->format, {k, v}, dtype, total, {k_token_stride, v_token_stride}, {k_head_stride, v_head_stride}, seqs, first, cu, n,
-                             most, s);
+                             most, ctx->sm_count, s);
         });
         return record_cuda(ctx, cudaGetLastError(), "eosq_kv8_store launch") ? EOSQ_ERR_CUDA : EOSQ_OK;
     });

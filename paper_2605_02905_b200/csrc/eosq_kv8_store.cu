@@ -302,7 +302,7 @@ void launch_store(const StoreArgs &a, dim3 grid, int chunks, cudaStream_t s) {
 }  // namespace
 
 void launch_kv8_store(const Kv8 &c, int fmt, const void *const (&x)[2], int dtype, long long total, const long long (&tok)[2],
-                      const long long (&head)[2], const int32_t *seqs, const int32_t *first, const int32_t *cu, int n, int max_new, cudaStream_t s) {
+                      const long long (&head)[2], const int32_t *seqs, const int32_t *first, const int32_t *cu, int n, int max_new, int sm_count, cudaStream_t s) {
     StoreArgs a;
     a.c = c;
     for (int kv = 0; kv < 2; ++kv) {
@@ -317,7 +317,7 @@ void launch_kv8_store(const Kv8 &c, int fmt, const void *const (&x)[2], int dtyp
     a.max_new = max_new;
     a.slots = (max_new + c.page_size() - 2) / c.page_size() + 1;
     // Of a page's heads, keys and values, so many CTAs' shares that there are eight CTAs per SM, if there are pages for fewer.
-    const long long pages = static_cast<long long>(n) * a.slots, wanted = (8ll * 148 + pages - 1) / pages;
+    const long long pages = static_cast<long long>(n) * a.slots, wanted = (8ll * sm_count + pages - 1) / pages;
     const dim3 grid(static_cast<unsigned>(pages), static_cast<unsigned>(std::min<long long>(2ll * c.heads, std::max(wanted, 2ll))));
     const int chunks = std::min(max_new, c.page_size()) << (c.d_shift - 3);
     auto go = [&](auto t) {
