@@ -199,8 +199,9 @@ int eosq_scores(eosq_ctx *ctx, const eosq_cache_t *kcache, int64_t num_kv_heads,
  *
  * Keys and values of tokens that no compressed block holds: the newest tokens of a sequence, the tokens that a
  * block is still being filled with, or an encoder's states.  (The paper keeps such tokens as they are, in an
- * fp16 tail buffer next to the compressed blocks.)  A number is held as one byte, its code; the tokens of a
- * page share, per KV head, one scale for their keys and one for their values: number = code * scale.
+ * fp16 tail buffer next to the compressed blocks.  No call turns pages into the blocks that eosq_encode takes.)
+ * A number is held as one byte, its code; the tokens of a page share, per KV head, one scale for their keys and
+ * one for their values: number = code * scale.
  *
  * Sequences own pages through a table in device memory; whole pages may be shared by several sequences (after
  * eosq_kv8_fork), a page that is not full belongs to one.  All state is plain device memory of the caller.

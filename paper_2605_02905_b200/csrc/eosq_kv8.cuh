@@ -283,7 +283,8 @@ constexpr int KV8_EXP_MIN = -126, KV8_EXP_MAX = 113;
 
 // Scores are base-2 logarithms; a weight is 2^(x - m + KV8_SHIFT), m being a running maximum that is only moved when a score passes
 // it by more than KV8_SLACK.  So weights are at most 2^14, inside fp16, and those of fp16's smallest normal numbers are 2^-20 of
-// the largest when m is exact.  x contains log2 of the page's value scale, so that the product with the codes of the values needs no
+// the largest when m is exact.  They are rounded to fp16 because the second product takes fp16 operands, which hold the codes of both formats exactly: half a step of 2^-11 each,
+// independent of one another, while their sum is of the weights before that, in fp32.  x contains log2 of the page's value scale, so that the product with the codes of the values needs no
 // scaling; the sum of the weights takes it out again.
 constexpr float KV8_SHIFT = 6.0f, KV8_SLACK = 8.0f;
 // Base-2 logarithms beyond 2^22 are so far apart in fp32 that SHIFT - m, or a bound on them under one rounding, is off by whole powers of two of a weight: where a
@@ -497,6 +498,9 @@ inline bool kv8_few_rows(long long most, long long rows, int n, int d) { return 
 // Both, where a prompt's chunk comes with sequences that get a token each: entries of up to so many rows through the first and then the others through the second; 0: one
 // of them takes all.  8 heads, G = 4, d = 128, through one kernel / both: 63 single tokens on 4096 each and a chunk of 512 queries 347 / 168 us, with a chunk of 128
 // 179 / 139; 31 on 2000 and a chunk of 512 on 16000 231 / 201; 63 on 500 with one of 128 44 / 48, two more launches; 7 on 1000 with one of 128 51 / 54.
+// Chunks of fewer rows than that go through one kernel, mostly the first, by the mean.  On short contexts that is ahead, on long ones it is not: a call as it is / two calls,
+// of the single tokens and of the chunk, for a chunk of 16 and of 127 queries among 7 single tokens on 500 each 15 / 32 and 26 / 39 us, on 4096 33 / 44 and 60 / 59, on 32768 164 / 147
+// and 309 / 191; among 31 on 32768 485 / 377 and 862 / 421; among 63 on 4096 142 / 129 and 190 / 139.
 inline int kv8_split(long long most, long long rows, int n, int G) {
     if (most < 512 || rows > n * (most / 4) || G > 16) return 0;
     return G <= 8 ? 8 : 16;

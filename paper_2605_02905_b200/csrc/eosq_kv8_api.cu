@@ -169,7 +169,8 @@ extern "C" int eosq_kv8_attend(eosq_ctx *ctx, const eosq_kv8_t *cache, int layer
         // Rows of the table that hold few tokens: what CTAs could share of a row tile is less than joining it would cost, and the second kernel is not needed.
         // Shared and joined / whole, one query a sequence, 8 heads: 10.6 / 9.0 us at one sequence of 300 tokens, 15.3 / 11.8 at 19 of 440, 20.2 / 17.2 at 64
         // of 300, 16.7 / 16.8 at 64 of 1 to 500; 22.1 / 23.9 at 100 queries on 300 tokens and 25.6 / 22.4 at 300 queries.  With many row tiles to a CTA
-        // what is saved falls (52.6 / 48.2 at 256) and runs of long sequences would make some CTAs late.
+        // what is saved falls (52.6 / 48.2 at 256) and runs of long sequences would make some CTAs late.  (The sequences' lengths are in device memory: what is asked for here is the
+        // table's width, so short sequences in a wide table are shared out like long ones.)
         a.whole = static_cast<int64_t>(cache->max_pages) * cache->page_size <= 4 * KV8_KEYS && row_tiles * cache->kv_heads <= 8.0 * ctx->sm_count;
         a.total = total;
         a.q = q;

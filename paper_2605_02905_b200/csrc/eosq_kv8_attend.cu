@@ -18,7 +18,7 @@ namespace {
 // Both products have the tokens' side as the MMA's larger one: scores are (16 tokens) x (8 query rows), the sums (16 channels) x (8 rows).
 // A product of queries by keys (16 rows, half of them empty with up to 8 heads to a group) would take twice the MMAs, weights and registers: it was
 // 573 instructions for 16 tokens and 286 us for 16 x 32768 tokens.
-// What bounds it is the memory: those tokens, 8 heads of 128 with four queries each, take 167 us, 6.4 TB/s of codes (a copy reaches 6.46), with half the issue
+// What bounds it is the memory: those tokens, 8 heads of 128 with four queries each, take 168 us in a graph, 6.4 TB/s of codes (a copy reaches 6.46), with half the issue
 // slots in use.  Short of that it is the way to the first tile: 1.4 us (48 entries: 2.4) until a CTA knows its run, 1.3 for a page's number, as much for its scales, 2
 // for the codes, 2 for the queries, which wait behind other CTAs' codes; then 1 us a tile until the code has been fetched.  48 x 64 .. 8192 tokens: 40 us, 26.5 at a copy's rate.
 // Queries brought by the fetching warp with the codes gained 2 % there and lost 3 % at d = 64 and on one short sequence; codes asked for before

@@ -21,8 +21,8 @@ namespace {
 //   warps 14, 15     bring the next row tile's queries in as soon as this one's last scores have been made
 // A half's chain is what bounds it: products of 128 x 128 x d twice (some 1500 cycles, shared memory feeding them), then the weights of a row per thread (some 2500, of
 // which the special function units need 1024, or 2048 where the halves meet); the halves overlap, so a tile takes some 4800 cycles: four prompts
-// of 2048 queries on 12000 tokens run at 1014 TFLOP/s (1717 for a library product), four of 500 to 2048 on 2048 to 12000, with their diagonal and their
-// last row tiles, at 895.  Half the weights' 2^x by a polynomial
+// of 2048 queries on 12000 tokens run at 998 TFLOP/s (1717 for a library product), four of 500 to 2048 on 2048 to 12000, with their diagonal and their
+// last row tiles, at 888 (1004 and 893 while a turn was made again instead of looking at what is left of a tile, which did not end on some scores beyond 2^27).  Half the weights' 2^x by a polynomial
 // instead was slower, so were scores of 64 tokens with the next 64 beside them, and twice the warps for the codes.
 constexpr int ROWS = 256, HALF = 128, KEYS = KV8_KEYS, GROUP = KV8_GROUP, GROUPS = KV8_GROUPS;
 constexpr int LOADER = 8, ISSUER = 12, FETCHER = 13, THREADS = 32 * 16, STAGES = 2, INFOS = 4;
